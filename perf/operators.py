@@ -1,0 +1,452 @@
+"""The operators of a pruned decoder step, as a serving program calls them: a pruned layer with 4-bit weights and group
+scales (``pivot_qfc_run``), the root-mean-square norm with the residual's addition that stands before it and hands it its
+input in 8 bits (``pivot_norm_run``), and a mixture-of-experts layer for a few tokens whose experts are such layers
+(``pivot_moe_run``).
+
+Everything is given in block space, as ``pivot_qfc_plan`` takes it: codes 0..15, two to a byte (the even column in the low
+half), fp16 scales and, where there are some, zero points per row and group of columns, a mask of kept tiles and the two
+permutations.  A weight is ``scale * (code - zero)``, zero = 8 where none is given.  ``own`` says whether ``run`` goes through
+the library; the plain forms are elementary torch operations.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+
+# ------------------------------------------------------------------ cases
+
+def _qfc(M, K, bh, bw, group, kept, x, batch, zeros=False, perm=True, skew=False, act=0, name=None):
+    c = dict(kind="qfc", M=M, K=K, bh=bh, bw=bw, group=group, kept=kept, x=x, batch=batch, zeros=zeros, perm=perm, skew=skew,
+             act=act)
+    return dict(c, name=name) if name else c
+
+
+def _norm(rows, cols, x, res, out, perm=False, name=None):
+    c = dict(kind="norm", rows=rows, cols=cols, x=x, res=res, out=out, perm=perm)
+    return dict(c, name=name) if name else c
+
+
+def _moe(tokens, experts, top_k, D, F, bh, bw, group, kept, zeros=False, perm=False, renorm=True, name=None):
+    c = dict(kind="moe", tokens=tokens, experts=experts, top_k=top_k, D=D, F=F, bh=bh, bw=bw, group=group, kept=kept,
+             zeros=zeros, perm=perm, renorm=renorm)
+    return dict(c, name=name) if name else c
+
+
+def listed():
+    return [
+        # one request to a small classifier layer of ragged sizes: latency only
+        _qfc(1000, 1020, 16, 32, 32, 0.5, "f16", 1, act=1, name="qfc 1000x1020 f16 b1"),
+        # one request to a square layer that keeps every weight, as 4-bit checkpoints come
+        _qfc(4096, 4096, 64, 128, 128, 1.0, "f16", 1, perm=False, name="qfc 4096 dense f16 b1"),
+        # one request to the AlexNet fc6 shape, pruned, input in 8 bits and block order, as the norm leaves it
+        _qfc(4096, 9216, 32, 64, 64, 0.25, "q8", 1, zeros=True, name="qfc 4096x9216 q8 b1"),
+        # sixteen requests served together, sizes that fit no tile
+        _qfc(3999, 9203, 32, 32, 128, 0.5, "f16", 16, zeros=True, name="qfc 3999x9203 f16 b16"),
+        # a full batch, 8-bit input
+        _qfc(4096, 4096, 64, 64, 64, 0.5, "q8", 64, name="qfc 4096 q8 b64"),
+        # four requests to the largest matrix
+        _qfc(16384, 16384, 64, 64, 128, 1.0, "f16", 4, name="qfc 16384 f16 b4"),
+        # one row on its way into a 4-bit layer: latency only
+        _norm(1, 4096, "f32", "f32", "q8", perm=True, name="norm 1x4096 f32 q8"),
+        # a batch of ragged rows before fp16 layers
+        _norm(64, 9203, "f32", "f16", "f16", name="norm 64x9203 f32 f16"),
+        # the rows of a long prompt
+        _norm(8192, 4096, "f16", "f16", "q8", name="norm 8192x4096 f16 q8"),
+        # one token through two of eight large experts: bandwidth
+        _moe(1, 8, 2, 4096, 8192, 64, 128, 128, 1.0, name="moe 8 experts 1 token"),
+        # sixteen tokens through six of 64 small experts, which touch most of them
+        _moe(16, 64, 6, 2048, 1408, 64, 64, 64, 1.0, zeros=True, renorm=False, name="moe 64 experts 16 tokens"),
+        # four tokens through two of sixteen pruned experts, pivoted, sizes that fit no tile
+        _moe(4, 16, 2, 2040, 3000, 32, 32, 32, 0.25, perm=True, name="moe 16 pruned experts 4 tokens"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(("qfc", "qfc", "qfc", "norm", "moe", "moe"))
+    if kind == "norm":
+        cols = _log(rng, 1, 16384)
+        rows = min(_log(rng, 1, 8192), max(1, (1 << 25) // cols))
+        return _norm(rows, cols, rng.choice(("f16", "f32")), rng.choice(("f16", "f32", "none")),
+                     rng.choice(("f16", "f32", "q8", "q8")), perm=rng.random() < 0.3)
+    bh, bw, group = rng.choice((16, 32, 64)), rng.choice((32, 64, 128)), rng.choice((32, 64, 128))
+    kept = 1.0 if rng.random() < 0.4 else round(math.exp(rng.uniform(math.log(0.05), math.log(0.7))), 4)
+    zeros, perm = rng.random() < 0.5, rng.random() < 0.5
+    if kind == "qfc":
+        M, K = _log(rng, 64, 16384), _log(rng, 64, 16384)
+        if M * K > 1.2e8:
+            K = int(1.2e8 / M)
+        batch = 1 if rng.random() < 0.4 else _log(rng, 2, 64)
+        return _qfc(M, K, bh, bw, group, kept, rng.choice(("f16", "f16", "q8")), batch, zeros=zeros, perm=perm,
+                    skew=rng.random() < 0.3, act=rng.choice((0, 1)))
+    experts = _log(rng, 2, 64)
+    top_k = min(experts, rng.choice((1, 2, 2, 4, 6, 8)))
+    D = _log(rng, 256, 4096)
+    F = min(_log(rng, 128, 8192), int(2.4e8 / (experts * D)))
+    tokens = 1 if rng.random() < 0.4 else rng.randint(2, 16)
+    return _moe(tokens, experts, top_k, D, max(F, 64), bh, bw, group, kept, zeros=zeros, perm=perm, renorm=rng.random() < 0.5)
+
+
+# ------------------------------------------------------------------ inputs
+
+_TD = {"f16": torch.float16, "f32": torch.float32}
+
+
+class _State:
+    """What a program keeps between calls: its inputs, weights, plans, workspace and output buffers."""
+
+    def __init__(self, case, seed):
+        self.case = case
+        self.rng = np.random.default_rng(seed)
+        self.gen = torch.Generator(device="cuda")
+        self.gen.manual_seed(seed)
+        self.free = []
+
+    def __del__(self):
+        for destroy, handle in reversed(self.free):
+            destroy(handle)
+
+    def normal(self, *shape, sigma=1.0):
+        return torch.randn(*shape, generator=self.gen, device="cuda").mul_(sigma)
+
+    def integers(self, lo, hi, *shape):
+        return torch.randint(lo, hi, shape, generator=self.gen, device="cuda")
+
+    def permutation(self, n, perm, pairs=False):
+        """A random permutation or the identity; pairs: neighbours stay neighbours (the gate row and the up row of a unit)."""
+        if not perm:
+            return np.arange(n, dtype=np.int32)
+        if pairs:
+            p = self.rng.permutation(n // 2)
+            return np.stack([2 * p, 2 * p + 1], 1).reshape(-1).astype(np.int32)
+        return self.rng.permutation(n).astype(np.int32)
+
+    def mask(self, nbr, nbc, kept, skew=False):
+        """round(kept * tiles) kept tiles, anywhere; skew: block rows of very different lengths."""
+        n = int(round(kept * nbr * nbc))
+        key = self.rng.gumbel(size=(nbr, nbc))
+        if skew:
+            key += -0.7 * np.log(1.0 + self.rng.permutation(nbr))[:, None]
+        m = np.zeros(nbr * nbc, dtype=np.uint8)
+        m[np.argsort(-key.reshape(-1), kind="stable")[:n]] = 1
+        return m.reshape(nbr, nbc)
+
+    def layer(self, M, K, c, perm, prow=None, pcol=None, pairs=False):
+        """The weights of one layer, as a quantiser leaves them: codes of about normal weights, scales of N(0, 1/K) weights."""
+        bh, bw, G = c["bh"], c["bw"], c["group"]
+        w = torch.empty(M, K + (K & 1), dtype=torch.float16, device="cuda").normal_(8.0, 2.6, generator=self.gen)
+        w = w.round_().clamp_(0, 15).to(torch.uint8)
+        ng = -(-K // G)
+        L = dict(M=M, K=K, bh=bh, bw=bw, group=G, act=c.get("act", 0))
+        L["codes"] = w[:, 0::2] + 16 * w[:, 1::2]
+        L["scales"] = torch.rand(M, ng, generator=self.gen, device="cuda").add_(0.5).mul_(K ** -0.5 / 2.6).to(torch.float16)
+        L["zeros"] = self.integers(6, 11, M, ng).to(torch.uint8) if c["zeros"] else None
+        L["bias"] = self.normal(M, sigma=0.1)
+        L["mask"] = self.mask(-(-M // bh), -(-K // bw), c["kept"], c.get("skew", False))
+        L["prow"] = self.permutation(M, perm, pairs) if prow is None else prow
+        L["pcol"] = self.permutation(K, perm) if pcol is None else pcol
+        for k in ("mask", "prow", "pcol"):
+            L["t_" + k] = torch.from_numpy(L[k]).cuda().long()
+        return L
+
+    def plan(self, L):
+        from paper_1712_01084_amd import binding as B
+        host = lambda t: None if t is None else t.cpu().numpy()  # noqa: E731
+        p = B.pivot_qfc_plan(L["M"], L["K"], L["bh"], L["bw"], L["group"], host(L["codes"]), host(L["scales"]), host(L["zeros"]),
+                             L["mask"], L["prow"], L["pcol"], host(L["bias"]), act=L["act"], device=0)
+        self.free.append((B.pivot_qfc_plan_destroy, p))
+        return p
+
+    def workspace(self, nbytes):
+        from paper_1712_01084_amd import binding as B
+        self.nws = max(nbytes, 256)
+        self.ws = torch.empty(self.nws, dtype=torch.uint8, device="cuda")
+        B.pivot_workspace_init(self.ws.data_ptr(), self.nws, torch.cuda.current_stream().cuda_stream)
+
+
+def _prepare_qfc(c, seed):
+    s = _State(c, seed)
+    s.layer_ = s.layer(c["M"], c["K"], c, c["perm"])
+    s.sx = None
+    if c["x"] == "q8":
+        s.x = s.normal(c["batch"], c["K"], sigma=40.0).round_().clamp_(-127, 127).to(torch.int8)
+        s.sx = torch.rand(c["batch"], generator=s.gen, device="cuda").add_(0.5).mul_(0.025)
+    else:
+        s.x = s.normal(c["batch"], c["K"]).to(torch.float16)
+    s.y = torch.zeros(c["batch"], c["M"], device="cuda")
+    if own:                       # a program lays its weights out once
+        from paper_1712_01084_amd import binding as B
+        s.p = s.plan(s.layer_)
+        s.workspace(B.pivot_qfc_workspace_bytes(s.p, c["batch"]))
+    return s
+
+
+def _prepare_norm(c, seed):
+    s = _State(c, seed)
+    rows, cols = c["rows"], c["cols"]
+    s.x = s.normal(rows, cols).to(_TD[c["x"]])
+    s.res = None if c["res"] == "none" else s.normal(rows, cols, sigma=3.0).to(_TD[c["res"]])
+    s.weight = s.normal(cols, sigma=0.2).add_(1.0)
+    s.pcol = s.permutation(cols, c["perm"])
+    s.t_pcol = torch.from_numpy(s.pcol).cuda().long()
+    s.res_out = None if s.res is None else torch.zeros_like(s.res)
+    s.out = torch.zeros(rows, cols, dtype=torch.int8 if c["out"] == "q8" else _TD[c["out"]], device="cuda")
+    s.scale = torch.zeros(rows, device="cuda") if c["out"] == "q8" else None
+    s.p = None
+    if own and c["perm"]:         # the layer whose input the rows become: its column permutation is the order they are left in
+        z = dict(bh=16, bw=32, group=32, kept=0.0, zeros=False)
+        s.p = s.plan(s.layer(16, cols, z, False, pcol=s.pcol))
+    return s
+
+
+def _prepare_moe(c, seed):
+    s = _State(c, seed)
+    E, D, F = c["experts"], c["D"], c["F"]
+    drow = s.permutation(D, c["perm"])
+    s.gate_up = [s.layer(2 * F, D, c, c["perm"], pairs=True) for _ in range(E)]
+    s.down = [s.layer(D, F, c, c["perm"], prow=drow) for _ in range(E)]
+    s.router = s.normal(E, D, sigma=D ** -0.5).to(torch.float16)
+    s.x = s.normal(c["tokens"], D).to(torch.float16)
+    s.y = torch.zeros(c["tokens"], D, device="cuda")
+    s.ids = torch.zeros(c["tokens"], c["top_k"], dtype=torch.int32, device="cuda")
+    s.weights = torch.zeros(c["tokens"], c["top_k"], device="cuda")
+    if own:
+        from paper_1712_01084_amd import binding as B
+        s.p = B.pivot_moe_plan([s.plan(L) for L in s.gate_up], [s.plan(L) for L in s.down], c["top_k"], s.router.cpu().numpy(),
+                               renormalise=c["renorm"])
+        s.free.append((B.pivot_moe_plan_destroy, s.p))
+        s.workspace(B.pivot_moe_workspace_bytes(s.p, c["tokens"]))
+        s.gate_up = s.down = None
+    else:                         # the plain form works on all experts at once
+        s.gate_up, s.down = _stacked(s.gate_up), _stacked(s.down)
+    return s
+
+
+def _stacked(layers):
+    first = layers[0]
+    L = {k: first[k] for k in ("M", "K", "bh", "bw", "group", "act")}
+    for k in ("codes", "scales", "zeros", "bias", "t_mask", "t_prow", "t_pcol"):
+        L[k] = None if first[k] is None else torch.stack([l[k] for l in layers])
+    return L
+
+
+def prepare(case, seed):
+    return {"qfc": _prepare_qfc, "norm": _prepare_norm, "moe": _prepare_moe}[case["kind"]](case, seed)
+
+
+# ------------------------------------------------------------------ one pass
+
+def _weights(L, pick=None):
+    """[..., M, K] weights in block space, 32 bits; `pick`: of these layers of a stack."""
+    g = (lambda t: t) if pick is None else (lambda t: t[pick])
+    codes, M, K = g(L["codes"]), L["M"], L["K"]
+    w = torch.stack([codes & 15, codes >> 4], -1).flatten(-2)[..., :K].float()
+    zero = 8.0 if L["zeros"] is None else g(L["zeros"]).float().repeat_interleave(L["group"], -1)[..., :K]
+    w = (w - zero) * g(L["scales"]).float().repeat_interleave(L["group"], -1)[..., :K]
+    keep = g(L["t_mask"]).bool().repeat_interleave(L["bh"], -2)[..., :M, :].repeat_interleave(L["bw"], -1)[..., :K]
+    return torch.where(keep, w, torch.zeros((), device=w.device))
+
+
+def _plain_qfc(s):
+    c, L = s.case, s.layer_
+    xg = s.x.float() if c["x"] == "q8" else s.x.float()[:, L["t_pcol"]]
+    v = xg @ _weights(L).t()
+    if s.sx is not None:
+        v = v * s.sx[:, None]
+    v = v + L["bias"][L["t_prow"]]
+    y = torch.empty_like(v)
+    y[:, L["t_prow"]] = v.clamp(min=0) if c["act"] else v
+    return y
+
+
+def _own_qfc(s):
+    from paper_1712_01084_amd import binding as B
+    c = s.case
+    q8 = c["x"] == "q8"
+    B.pivot_qfc_run(s.p, s.x.data_ptr(), B.PIVOT_Q8 if q8 else B.PIVOT_F16, c["K"], s.sx.data_ptr() if q8 else None,
+                    s.y.data_ptr(), c["M"], c["batch"], s.ws.data_ptr(), s.nws, torch.cuda.current_stream().cuda_stream,
+                    flags=B.PIVOT_QFC_X_BLOCK_ORDER if q8 else 0)
+    return s.y
+
+
+def _plain_norm(s):
+    c = s.case
+    wide = torch.float64 if c["out"] == "q8" else torch.float32     # a value next to the middle of two codes
+    h = s.x.to(wide)
+    if s.res is not None:
+        h = h + s.res.to(wide)
+    rstd = 1.0 / torch.sqrt((h * h).mean(1, keepdim=True) + 1e-6)
+    hw = (h * s.weight.to(wide))[:, s.t_pcol]
+    out = {} if s.res is None else {"res": h.to(s.res.dtype)}
+    if c["out"] != "q8":
+        out["out"] = (hw * rstd).to(s.out.dtype)
+        return out
+    most = hw.abs().amax(1, keepdim=True)
+    code = torch.round(hw * torch.where(most > 0, 127.0 / most, torch.zeros_like(most))).to(torch.int8)
+    out["out"] = code * (most * rstd / 127.0).float()
+    return out
+
+
+def _own_norm(s):
+    from paper_1712_01084_amd import binding as B
+    c = s.case
+    kinds = {"f32": B.PIVOT_F32, "f16": B.PIVOT_F16, "q8": B.PIVOT_Q8}
+    n = c["cols"]
+    B.pivot_norm_run(s.x.data_ptr(), kinds[c["x"]], n, s.out.data_ptr(), kinds[c["out"]], n, c["rows"], n,
+                     weight_ptr=s.weight.data_ptr(), eps=1e-6,
+                     res_ptr=None if s.res is None else s.res.data_ptr(), rtype=kinds.get(c["res"], B.PIVOT_F32), ldr=n,
+                     res_out_ptr=None if s.res is None else s.res_out.data_ptr(), ldro=n,
+                     scale_ptr=None if s.scale is None else s.scale.data_ptr(), order=s.p,
+                     stream=torch.cuda.current_stream().cuda_stream)
+    out = {} if s.res is None else {"res": s.res_out}
+    out["out"] = s.out if s.scale is None else s.out * s.scale[:, None]
+    return out
+
+
+def _plain_moe(s):
+    c = s.case
+    T, E, k, F = c["tokens"], c["experts"], c["top_k"], c["F"]
+    x = s.x.float()
+    logits = x @ s.router.float().t()
+    prob = torch.exp(logits - logits.amax(1, keepdim=True))
+    prob = prob / prob.sum(1, keepdim=True)
+    ids = torch.sort(logits, dim=1, descending=True, stable=True)[1][:, :k]      # ties: the lowest index
+    p = torch.gather(prob, 1, ids)
+    if c["renorm"]:
+        p = p / p.sum(1, keepdim=True)
+    if T * k <= E:                # fewer (token, expert) pairs than experts: only their experts
+        pick, xs = ids.reshape(-1), x.repeat_interleave(k, 0)[:, None, :]
+        share = torch.zeros(T * k, T, device="cuda")
+        share[torch.arange(T * k, device="cuda"), torch.arange(T, device="cuda").repeat_interleave(k)] = p.reshape(-1)
+        share = share[:, :, None]
+    else:                         # every expert on every token
+        pick, xs = torch.arange(E, device="cuda"), x[None].expand(E, T, c["D"])
+        share = torch.zeros(T, E, device="cuda").scatter_(1, ids, p).t()[:, :, None]
+    up, down = s.gate_up, s.down
+    n, rows = len(pick), xs.shape[1]
+    xg = torch.gather(xs, 2, up["t_pcol"][pick][:, None, :].expand(n, rows, c["D"]))
+    v = torch.matmul(xg, _weights(up, pick).transpose(1, 2).contiguous())
+    z = torch.empty_like(v).scatter_(2, up["t_prow"][pick][:, None, :].expand_as(v), v) + up["bias"][pick][:, None, :]
+    z = z.reshape(n, rows, F, 2)  # the gate's row and the up row of a unit lie side by side
+    h = z[..., 0] / (1.0 + torch.exp(-z[..., 0])) * z[..., 1]
+    hg = torch.gather(h, 2, down["t_pcol"][pick][:, None, :].expand(n, rows, F))
+    v = torch.matmul(hg, _weights(down, pick).transpose(1, 2).contiguous())
+    d = torch.empty_like(v).scatter_(2, down["t_prow"][pick][:, None, :].expand_as(v), v) + down["bias"][pick][:, None, :]
+    y = (share * d).sum(0) if rows == T else (share * d.expand(n, T, c["D"])).sum(0)
+    return {"y": y, "ids": ids.to(torch.int32), "weights": p}
+
+
+def _own_moe(s):
+    from paper_1712_01084_amd import binding as B
+    c = s.case
+    B.pivot_moe_run(s.p, s.x.data_ptr(), c["D"], s.y.data_ptr(), c["D"], c["tokens"], s.ws.data_ptr(), s.nws,
+                    torch.cuda.current_stream().cuda_stream, ids_ptr=s.ids.data_ptr(), weights_ptr=s.weights.data_ptr())
+    return {"y": s.y, "ids": s.ids, "weights": s.weights}
+
+
+def run(state):
+    kind = state.case["kind"]
+    if own:
+        return {"qfc": _own_qfc, "norm": _own_norm, "moe": _own_moe}[kind](state)
+    return {"qfc": _plain_qfc, "norm": _plain_norm, "moe": _plain_moe}[kind](state)
+
+
+# ------------------------------------------------------------------ 64 bits
+
+def _matrix64(M, K, c, codes, scales, zeros, mask, prow, pcol):
+    """The layer's matrix in natural coordinates, in 64 bits."""
+    W = torch.zeros(M, codes.shape[1] * 2, dtype=torch.float64, device="cuda")
+    W[:, 0::2] = (codes % 16).double()
+    W[:, 1::2] = torch.div(codes, 16, rounding_mode="floor").double()
+    W = W[:, :K]
+    group = torch.arange(K, device="cuda") // c["group"]
+    W = W - (zeros.double()[:, group] if zeros is not None else 8.0)
+    W = W * scales.double()[:, group]
+    W = W * (mask.double()[torch.arange(M, device="cuda") // c["bh"]])[:, torch.arange(K, device="cuda") // c["bw"]]
+    natural = torch.empty_like(W)
+    natural[prow[:, None], pcol[None, :]] = W
+    return natural
+
+
+def _exact_qfc(s, c):
+    L = s.layer_
+    W = _matrix64(c["M"], c["K"], c, L["codes"], L["scales"], L["zeros"], L["t_mask"], L["t_prow"], L["t_pcol"])
+    x = s.x.double()
+    if c["x"] == "q8":            # comes in block order
+        natural = torch.empty_like(x)
+        natural[:, L["t_pcol"]] = x
+        x = natural * s.sx.double()[:, None]
+    y = torch.matmul(x, W.t()) + L["bias"].double()
+    return torch.relu(y) if c["act"] else y
+
+
+def _exact_norm(s, c):
+    h = s.x.double() + (0.0 if s.res is None else s.res.double())
+    out = {} if s.res is None else {"res": h}
+    n = torch.index_select(h * s.weight.double() * torch.rsqrt(h.square().sum(1) / c["cols"] + 1e-6)[:, None], 1, s.t_pcol)
+    if c["out"] == "q8":
+        step = n.abs().max(1)[0][:, None] / 127.0
+        n = torch.where(step > 0, torch.round(n / torch.where(step > 0, step, torch.ones_like(step))), torch.zeros_like(n)) * step
+    out["out"] = n
+    return out
+
+
+def _exact_moe(s, c):
+    T, E, k, F, D = c["tokens"], c["experts"], c["top_k"], c["F"], c["D"]
+    x, y = s.x.double(), torch.zeros(T, D, dtype=torch.float64, device="cuda")
+    logits = (x @ s.router.double().t()).cpu().numpy()
+    ids = np.argsort(-logits, axis=1, kind="stable")[:, :k]
+    e = np.exp(logits - logits.max(1, keepdims=True))
+    p = np.take_along_axis(e, ids, 1) / (np.take_along_axis(e, ids, 1).sum(1, keepdims=True) if c["renorm"] else e.sum(1, keepdims=True))
+
+    def matrix(L, M, K, i):
+        return _matrix64(M, K, c, L["codes"][i], L["scales"][i], None if L["zeros"] is None else L["zeros"][i], L["t_mask"][i],
+                         L["t_prow"][i], L["t_pcol"][i])
+
+    for i in sorted(set(ids.reshape(-1).tolist())):
+        t, j = np.nonzero(ids == i)
+        tt = torch.from_numpy(t).cuda()
+        z = x[tt] @ matrix(s.gate_up, 2 * F, D, i).t() + s.gate_up["bias"][i].double()
+        gate, up = z[:, 0::2], z[:, 1::2]
+        h = gate * torch.sigmoid(gate) * up
+        d = h @ matrix(s.down, D, F, i).t() + s.down["bias"][i].double()
+        y.index_add_(0, tt, d * torch.from_numpy(p[t, j]).cuda()[:, None])
+    return {"y": y, "ids": None, "weights": torch.from_numpy(p)}
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"qfc": _exact_qfc, "norm": _exact_norm, "moe": _exact_moe}[case["kind"]](s, case)
+
+
+# ------------------------------------------------------------------ the floor
+
+def _layer_bytes(M, K, c):
+    """Half a byte per kept weight, its share of a group's scale and zero point, the tiles' columns, both permutations, bias."""
+    nbr, nbc = -(-M // c["bh"]), -(-K // c["bw"])
+    tiles = int(round(c["kept"] * nbr * nbc))
+    kept = min(tiles * c["bh"] * c["bw"], M * K)
+    return kept * (0.5 + (3.0 if c["zeros"] else 2.0) / c["group"]) + 4 * tiles + 4 * M + (4 * (M + K) if c["perm"] else 0), kept
+
+
+def work(case):
+    c = case
+    if c["kind"] == "qfc":
+        b, kept = _layer_bytes(c["M"], c["K"], c)
+        return {"bytes": b + c["batch"] * (c["K"] * (1 if c["x"] == "q8" else 2) + 4 * c["M"]), "flops": 2 * kept * c["batch"]}
+    if c["kind"] == "norm":
+        size = {"f32": 4, "f16": 2, "q8": 1, "none": 0}
+        n = c["rows"] * c["cols"]
+        return {"bytes": n * (size[c["x"]] + 2 * size[c["res"]] + size[c["out"]]) + 4 * c["cols"], "flops": 8 * n}
+    T, E, k = c["tokens"], c["experts"], c["top_k"]
+    active = E * (1.0 - (1.0 - k / E) ** T)          # experts that T tokens touch, on average
+    bu, ku = _layer_bytes(2 * c["F"], c["D"], c)
+    bd, kd = _layer_bytes(c["D"], c["F"], c)
+    return {"bytes": active * (bu + bd) + E * c["D"] * 2 + T * c["D"] * 6,
+            "flops": 2 * T * k * (ku + kd) + 2 * T * E * c["D"]}
