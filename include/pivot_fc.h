@@ -417,6 +417,162 @@ int    pivot_lstm_run(const pivot_fc_plan_t* plan, int H, int I, const void* xs_
                       void* ws_dev, size_t ws_bytes, void* stream);
 
 /*
+ * Layers with 4-bit weights.  The same layer as above, y = act(P_r^T * BSR(W') * (P_c x) + b), its kept tiles
+ * stored as 4-bit codes with an fp16 scale (and, optionally, a zero point) per row and group of columns:
+ *
+ *     W'[r][c] = scale[r][c / group] * (code[r][c] - zero[r][c / group]),      zero = 8 without zero points
+ *
+ * Everything is in block space, groups of columns too: weights are quantised after pivoting (with identity
+ * permutations, natural and block space are the same).
+ *
+ *   codes      host, M rows of ceil(K/2) bytes: two columns to a byte, the even one in the low half
+ *   scales     host, M * ceil(K/group) fp16 values
+ *   zeros      host, M * ceil(K/group) bytes 0..15, or NULL (= 8)
+ *   tile_mask  host, nbr*nbc bytes, or NULL (every tile is kept)
+ *   prow, pcol host, or NULL (identity)
+ *   bias       host, M floats in natural output coordinates, or NULL (= 0)
+ *
+ * bh is 16, 32 or 64; bw and group are 32, 64 or 128; M at most 2^22, K at most 65535.  A group may span several
+ * tiles and a tile several groups.  device = -1 makes a host-only plan (the schedule, for inspection).
+ */
+#define PIVOT_Q8 2   /* 8-bit integers in two's complement, one fp32 scale per row of x */
+
+typedef struct pivot_qfc_desc {
+    int32_t M, K, bh, bw;
+    int32_t group;         /* columns per scale                                                        */
+    int32_t act;           /* PIVOT_ACT_*                                                              */
+    int32_t chunk_blocks;  /* most blocks of 128 kept columns per work item; 0 = the library chooses:
+                            * whole block rows unless those leave compute units idle or their lengths
+                            * are very uneven                                                          */
+    int32_t device;        /* HIP device ordinal, or -1                                                */
+    int32_t flags;         /* 0                                                                        */
+} pivot_qfc_desc;
+
+typedef struct pivot_qfc_plan pivot_qfc_plan_t;
+
+/* The schedule of a plan (valid until the plan is destroyed).  The kept tiles of a block row, side by side, are cut
+ * into blocks of 128 columns (the last one filled up); `pieces` gives for each bw columns of a block the first
+ * block-space column they come from, or -1.  `chunks`: (block row, first block, end, first slot of the row, pieces
+ * of the row, slot, 0, 0), longest first.  The sums of a block row in several pieces are added in ascending slot order. */
+typedef struct pivot_qfc_view {
+    int32_t M, K, bh, bw, group, act, nbr, nbc, M_pad, K_pad, T, blocks, chunk_blocks, nchunks, groups_per_block;
+    const int32_t* row_ptr;    /* [nbr+1] kept tiles before block row i */
+    const int32_t* col_idx;    /* [T] */
+    const int32_t* block_ptr;  /* [nbr+1] blocks before block row i */
+    const int32_t* pieces;     /* [blocks * 128/bw] */
+    const int32_t* chunks;     /* [nchunks][8] */
+} pivot_qfc_view;
+
+int    pivot_qfc_plan(const pivot_qfc_desc* desc, const uint8_t* codes, const void* scales, const uint8_t* zeros,
+                      const uint8_t* tile_mask, const int32_t* prow, const int32_t* pcol, const float* bias,
+                      pivot_qfc_plan_t** out);
+int    pivot_qfc_plan_host_view(const pivot_qfc_plan_t* plan, pivot_qfc_view* view);
+void   pivot_qfc_plan_destroy(pivot_qfc_plan_t* plan);   /* NULL-safe */
+/* Scratch for `batch` rows, used under the rules of pivot_fc_workspace_bytes. */
+size_t pivot_qfc_workspace_bytes(const pivot_qfc_plan_t* plan, int batch);
+
+/*
+ * pivot_qfc_run - one application of the layer.
+ *
+ *   x_dev      device, [batch][K], row stride ldx elements: PIVOT_F16, or PIVOT_Q8 with xscale_dev ([batch] fp32:
+ *              x = xscale * integer), which pivot_norm_run makes.  In natural coordinates, or with
+ *              PIVOT_QFC_X_BLOCK_ORDER in the plan's block order (column c holds natural column pcol[c])
+ *   xscale_dev NULL for PIVOT_F16
+ *   y_dev      device, [batch][M] fp32, row stride ldy elements, natural coordinates; shares no memory with x
+ *   batch      1..64
+ *
+ * Sums are fp32, the integer products of a group with 8-bit inputs exact; repeated runs give identical bits.
+ */
+#define PIVOT_QFC_X_BLOCK_ORDER 1
+int    pivot_qfc_run(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, int64_t ldx, const float* xscale_dev,
+                     float* y_dev, int64_t ldy, int batch, int flags, void* ws_dev, size_t ws_bytes, void* stream);
+/* Name of the kernel instantiation pivot_qfc_run launches for this type of x and batch.  Needs no device. */
+int    pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch, char* buf, size_t buf_len);
+
+/*
+ * pivot_norm_run - root-mean-square norm of rows, with the residual's addition in front:
+ *
+ *     h = x + res        res_out = h        out = weight * h / sqrt(mean(h^2) + eps)
+ *
+ * What stands before a layer in a network of residual blocks.  h is not rounded before it is normalised (res_out is,
+ * to its type).  With otype PIVOT_Q8 a row comes out as 8-bit integers and one scale, as pivot_qfc_run takes it:
+ * scale = max |out| / 127, integer = out / scale rounded to nearest, ties to even, computed in 64 bits.  A row of
+ * zeros gives scale 0 and integers 0; a row with an infinity or NaN gives scale NaN and integers 0.
+ *
+ *   x          device, [rows][cols], PIVOT_F32 or PIVOT_F16, row stride ldx elements
+ *   res        device, [rows][cols], rtype PIVOT_F32 or PIVOT_F16, or NULL (= 0)
+ *   res_out    device, [rows][cols] of rtype, or NULL; may be res itself, else shares no memory with an input.
+ *              Needs res
+ *   weight     device, [cols] fp32, or NULL (= 1)
+ *   out        device, [rows][cols], PIVOT_F32, PIVOT_F16 or PIVOT_Q8; shares no memory with the others
+ *   scale      device, [rows] fp32; PIVOT_Q8 only
+ *   order      a plan with K = cols: the rows of out are left in its block order, so that its run need not gather
+ *              (PIVOT_QFC_X_BLOCK_ORDER); or NULL
+ * rows >= 1, cols 1..65535.  Needs no workspace.
+ */
+typedef struct pivot_norm_args {
+    const void* x; int64_t ldx;
+    const void* res; int64_t ldr;
+    void* res_out; int64_t ldro;
+    const float* weight;
+    void* out; int64_t ldo;
+    float* scale;
+    const pivot_qfc_plan_t* order;
+    int32_t xtype, rtype, otype, rows, cols;
+    float eps;
+} pivot_norm_args;
+int    pivot_norm_run(const pivot_norm_args* args, void* stream);
+
+/*
+ * A mixture-of-experts layer for a few tokens.  Per token x: logits = router x + router_bias; the top_k experts with
+ * the largest logits (ties: the lowest index); their weights are the softmax over all experts, or with
+ * PIVOT_MOE_RENORMALISE over the chosen ones; and
+ *
+ *     y = sum over chosen e of weight_e * down_e( silu(gate_e x) * (up_e x) )
+ *
+ * An expert is two layers with 4-bit weights, borrowed from the caller (they must outlive the plan): gate_up, 2F x D,
+ * whose natural rows 2u and 2u+1 are the gate and the up row of unit u, and down, D x F.  As in a chain, the
+ * permutations between the two are composed when the plan is made, and the first stores its activations in the block
+ * order of the second.  So that a unit's two rows meet in one work item, gate_up's row permutation keeps such pairs
+ * together (prow[2i] even, prow[2i+1] = prow[2i] + 1); so that the experts' outputs are summed where they lie, the
+ * down layers share one row permutation.  All gate_up plans share tile shape, group and whether they have zero
+ * points, all down plans likewise; none has an activation.
+ *
+ * A router_bias of -infinity switches an expert off.  A token with fewer than top_k experts left uses those (its
+ * other ids are -1, their weights 0), one with none gets y = 0.  A token whose logits hold a NaN gets y = NaN.
+ * Activations between the two layers are kept as fp16 value and remainder (22 bits); beyond the range of fp16 they
+ * are infinite.
+ */
+typedef struct pivot_moe_plan pivot_moe_plan_t;
+#define PIVOT_MOE_RENORMALISE 1
+typedef struct pivot_moe_desc {
+    int32_t experts;       /* 1..256 */
+    int32_t top_k;         /* 1..8, at most experts */
+    int32_t router_type;   /* PIVOT_F32 or PIVOT_F16 */
+    int32_t flags;
+    float   norm_eps;
+} pivot_moe_desc;
+
+/*   router       host, [experts][D] of router_type
+ *   router_bias  host, [experts] fp32, or NULL
+ *   norm_weight  host, [D] fp32: the layer begins with pivot_norm_run's norm with these weights and norm_eps, whose
+ *                output, rounded to fp16, is the tokens' x; or NULL (x as given)                                    */
+int    pivot_moe_plan(const pivot_moe_desc* desc, const pivot_qfc_plan_t* const* gate_up, const pivot_qfc_plan_t* const* down,
+                      const void* router, const float* router_bias, const float* norm_weight, pivot_moe_plan_t** out);
+void   pivot_moe_plan_destroy(pivot_moe_plan_t* plan);
+size_t pivot_moe_workspace_bytes(const pivot_moe_plan_t* plan, int tokens);
+/*   x_dev    device, [tokens][D], row stride ldx elements: PIVOT_F16; of plans with a norm PIVOT_F32 or PIVOT_F16
+ *   res_dev  plans with a norm only: device, [tokens][D] of xtype, row stride ldx; x is added to it before the norm
+ *            and the sum left there; or NULL
+ *   y_dev    device, [tokens][D] fp32, row stride ldy; shares no memory with x or res
+ *   tokens   1..16
+ *   ids, weights  device, [tokens][top_k] int32 and fp32, largest logit first, or NULL
+ * Uses the workspace under the rules of pivot_fc_workspace_bytes.  Repeated runs give identical bits. */
+int    pivot_moe_run(const pivot_moe_plan_t* plan, const void* x_dev, int xtype, int64_t ldx, void* res_dev,
+                     float* y_dev, int64_t ldy, int tokens, int32_t* ids_dev, float* weights_dev,
+                     void* ws_dev, size_t ws_bytes, void* stream);
+
+/*
  * The dense comparator: y = act(W x + b) with the full M x K matrix streamed
  * by this library's own dense kernel (the denominator of "speedup vs dense",
  * Section 5.1).  W_dev [M][K] of wdtype row-major, x_dev [batch][K] of

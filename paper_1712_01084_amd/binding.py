@@ -12,7 +12,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpivotfc.so")
 
-PIVOT_F32, PIVOT_F16 = 0, 1
+PIVOT_F32, PIVOT_F16, PIVOT_Q8 = 0, 1, 2
 PIVOT_BRC, PIVOT_BCR, PIVOT_CBR = 0, 1, 2
 PIVOT_PLAN_GATHER_FROM_GLOBAL = 1
 PIVOT_PLAN_LSTM_LAUNCH_PER_STEP = 2
@@ -23,6 +23,8 @@ PIVOT_ACT_NONE, PIVOT_ACT_RELU = 0, 1
 PIVOT_W_NATURAL, PIVOT_W_PIVOTED = 0, 1
 PIVOT_MLP_KEEP_FINAL_BLOCK_ORDER = 1
 PIVOT_MLP_LAUNCH_PER_LAYER = 2
+PIVOT_QFC_X_BLOCK_ORDER = 1
+PIVOT_MOE_RENORMALISE = 1
 
 PIVOT_OK = 0
 PIVOT_E_NULL, PIVOT_E_SHAPE, PIVOT_E_NOT_PERMUTATION, PIVOT_E_UNSUPPORTED = -1, -2, -3, -4
@@ -36,6 +38,8 @@ EXPORTS = [
     "pivot_mlp_workspace_bytes", "pivot_mlp_run", "pivot_mlp_kernel_name", "pivot_mlp_status", "pivot_mlp_status_word",
     "pivot_lstm_workspace_bytes", "pivot_lstm_run", "pivot_lstm_status", "pivot_lstm_status_word", "pivot_lstm_restore", "pivot_lstm_kernel_name",
     "pivot_dense_run", "pivot_csr_run", "pivot_null_run", "pivot_stream_read_run", "pivot_exchange_probe_run", "pivot_feedback_search",
+    "pivot_qfc_plan", "pivot_qfc_plan_host_view", "pivot_qfc_plan_destroy", "pivot_qfc_workspace_bytes", "pivot_qfc_run", "pivot_qfc_kernel_name",
+    "pivot_norm_run", "pivot_moe_plan", "pivot_moe_plan_destroy", "pivot_moe_workspace_bytes", "pivot_moe_run",
 ]
 
 
@@ -67,6 +71,27 @@ class pivot_mlp_view(C.Structure):
     _fields_ = [("L", C.c_int32), ("flags", C.c_int32),
                 ("q", C.POINTER(C.POINTER(C.c_int32))), ("dst", C.POINTER(C.POINTER(C.c_int32))),
                 ("identity", C.POINTER(C.c_int32)), ("one_launch", C.c_int32)]
+
+
+class pivot_qfc_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("M", "K", "bh", "bw", "group", "act", "chunk_blocks", "device", "flags")]
+
+
+class pivot_qfc_view(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("M", "K", "bh", "bw", "group", "act", "nbr", "nbc", "M_pad", "K_pad", "T", "blocks",
+                                          "chunk_blocks", "nchunks", "groups_per_block")]
+                + [(n, C.POINTER(C.c_int32)) for n in ("row_ptr", "col_idx", "block_ptr", "pieces", "chunks")])
+
+
+class pivot_norm_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ldx", C.c_int64), ("res", C.c_void_p), ("ldr", C.c_int64), ("res_out", C.c_void_p),
+                ("ldro", C.c_int64), ("weight", C.c_void_p), ("out", C.c_void_p), ("ldo", C.c_int64), ("scale", C.c_void_p),
+                ("order", C.c_void_p), ("xtype", C.c_int32), ("rtype", C.c_int32), ("otype", C.c_int32), ("rows", C.c_int32),
+                ("cols", C.c_int32), ("eps", C.c_float)]
+
+
+class pivot_moe_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("experts", "top_k", "router_type", "flags")] + [("norm_eps", C.c_float)]
 
 
 _lib = None
@@ -126,6 +151,21 @@ def lib():
     L.pivot_exchange_probe_run.argtypes = [vp, sz, C.c_int, vp]
     L.pivot_feedback_search.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, C.POINTER(C.c_double)]
     L.pivot_csr_run.argtypes = [vp, vp, vp, i32, i32, i64, vp, vp, vp, i32, vp]
+    L.pivot_qfc_plan.argtypes = [C.POINTER(pivot_qfc_desc), vp, vp, vp, vp, vp, vp, vp, C.POINTER(vp)]
+    L.pivot_qfc_plan_host_view.argtypes = [vp, C.POINTER(pivot_qfc_view)]
+    L.pivot_qfc_plan_destroy.argtypes = [vp]
+    L.pivot_qfc_plan_destroy.restype = None
+    L.pivot_qfc_workspace_bytes.argtypes = [vp, i32]
+    L.pivot_qfc_workspace_bytes.restype = sz
+    L.pivot_qfc_run.argtypes = [vp, vp, i32, i64, vp, vp, i64, i32, i32, vp, sz, vp]
+    L.pivot_qfc_kernel_name.argtypes = [vp, i32, i32, C.c_char_p, sz]
+    L.pivot_norm_run.argtypes = [C.POINTER(pivot_norm_args), vp]
+    L.pivot_moe_plan.argtypes = [C.POINTER(pivot_moe_desc), C.POINTER(vp), C.POINTER(vp), vp, vp, vp, C.POINTER(vp)]
+    L.pivot_moe_plan_destroy.argtypes = [vp]
+    L.pivot_moe_plan_destroy.restype = None
+    L.pivot_moe_workspace_bytes.argtypes = [vp, i32]
+    L.pivot_moe_workspace_bytes.restype = sz
+    L.pivot_moe_run.argtypes = [vp, vp, i32, i64, vp, vp, i64, i32, vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -348,3 +388,104 @@ def pivot_feedback_search(absW, levels, prow0, pcol0, max_iter=50):
     _check(lib().pivot_feedback_search(_np_ptr(absW), M, K, levels, max_iter, _np_ptr(prow0), _np_ptr(pcol0),
                                        _np_ptr(prow), _np_ptr(pcol), C.byref(mass)))
     return prow, pcol, mass.value
+
+
+def _array(a, dtype, shape, name):
+    """`a` as the library reads it; a wrong size is refused here, where it is known."""
+    if a is None:
+        return None
+    a = np.ascontiguousarray(a, dtype=dtype)
+    if a.shape != tuple(shape):
+        raise PivotError(PIVOT_E_SHAPE, "%s has shape %s, not %s" % (name, a.shape, tuple(shape)))
+    return a
+
+
+def pivot_qfc_plan(M, K, bh, bw, group, codes, scales, zeros=None, tile_mask=None, prow=None, pcol=None, bias=None, *,
+                   act=PIVOT_ACT_NONE, chunk_blocks=0, device=-1, flags=0):
+    """Host numpy arrays in (codes: [M][ceil(K/2)] bytes, scales: [M][ceil(K/group)] fp16), opaque plan handle out."""
+    d = pivot_qfc_desc(M, K, bh, bw, group, act, chunk_blocks, device, flags)
+    if min(M, K, bh, bw, group) > 0:      # the library refuses the rest
+        ng = -(-K // group)
+        codes = _array(codes, np.uint8, (M, -(-K // 2)), "codes")
+        scales = _array(scales, np.float16, (M, ng), "scales")
+        zeros = _array(zeros, np.uint8, (M, ng), "zeros")
+        tile_mask = _array(tile_mask, np.uint8, (-(-M // bh), -(-K // bw)), "tile_mask")
+        prow, pcol = _array(prow, np.int32, (M,), "prow"), _array(pcol, np.int32, (K,), "pcol")
+        bias = _array(bias, np.float32, (M,), "bias")
+    out = C.c_void_p()
+    _check(lib().pivot_qfc_plan(C.byref(d), _np_ptr(codes), _np_ptr(scales), _np_ptr(zeros), _np_ptr(tile_mask), _np_ptr(prow),
+                                _np_ptr(pcol), _np_ptr(bias), C.byref(out)))
+    return out
+
+
+def pivot_qfc_plan_host_view(plan):
+    """Copies of the plan's schedule as numpy arrays."""
+    v = pivot_qfc_view()
+    _check(lib().pivot_qfc_plan_host_view(plan, C.byref(v)))
+    out = {n: getattr(v, n) for n, t in v._fields_ if t is C.c_int32}
+    sizes = dict(row_ptr=v.nbr + 1, col_idx=v.T, block_ptr=v.nbr + 1, pieces=v.blocks * (128 // v.bw), chunks=v.nchunks * 8)
+    for n, size in sizes.items():
+        out[n] = np.ctypeslib.as_array(getattr(v, n), shape=(size,)).copy() if size else np.zeros(0, np.int32)
+    out["chunks"] = out["chunks"].reshape(-1, 8)
+    return out
+
+
+def pivot_qfc_plan_destroy(plan):
+    lib().pivot_qfc_plan_destroy(plan)
+
+
+def pivot_qfc_workspace_bytes(plan, batch):
+    return int(lib().pivot_qfc_workspace_bytes(plan, batch))
+
+
+def pivot_qfc_run(plan, x_ptr, xtype, ldx, xscale_ptr, y_ptr, ldy, batch, ws_ptr, ws_bytes, stream=None, *, flags=0):
+    _check(lib().pivot_qfc_run(plan, x_ptr, xtype, ldx, xscale_ptr, y_ptr, ldy, batch, flags, ws_ptr, ws_bytes, stream))
+
+
+def pivot_qfc_kernel_name(plan, xtype, batch):
+    """Name of the kernel instantiation pivot_qfc_run launches for this plan, type of x and batch."""
+    buf = C.create_string_buffer(256)
+    _check(lib().pivot_qfc_kernel_name(plan, xtype, batch, buf, 256))
+    return buf.value.decode()
+
+
+def pivot_norm_run(x_ptr, xtype, ldx, out_ptr, otype, ldo, rows, cols, *, weight_ptr=None, eps=1e-6, res_ptr=None, rtype=PIVOT_F32,
+                   ldr=0, res_out_ptr=None, ldro=0, scale_ptr=None, order=None, stream=None):
+    a = pivot_norm_args(x_ptr, ldx, res_ptr, ldr, res_out_ptr, ldro, weight_ptr, out_ptr, ldo, scale_ptr, order, xtype, rtype, otype,
+                        rows, cols, eps)
+    _check(lib().pivot_norm_run(C.byref(a), stream))
+
+
+def pivot_moe_plan(gate_up, down, top_k, router, *, router_bias=None, norm_weight=None, norm_eps=1e-6, renormalise=False, flags=0):
+    """Expert plans (pivot_qfc_plan) and the router's matrix, [experts][D] fp32 or fp16 numpy; opaque plan handle out."""
+    n = len(gate_up)
+    if len(down) != n:
+        raise PivotError(PIVOT_E_SHAPE, "%d gate_up and %d down plans" % (n, len(down)))
+    router = np.ascontiguousarray(router)
+    if router.dtype not in (np.float32, np.float16):
+        raise PivotError(PIVOT_E_UNSUPPORTED, "the router's matrix must be fp32 or fp16")
+    if n:
+        D = pivot_qfc_plan_host_view(gate_up[0])["K"]
+        router = _array(router, router.dtype, (n, D), "router")
+        router_bias = _array(router_bias, np.float32, (n,), "router_bias")
+        norm_weight = _array(norm_weight, np.float32, (D,), "norm_weight")
+    handles = [(C.c_void_p * max(n, 1))(*[p.value if isinstance(p, C.c_void_p) else p for p in ps]) for ps in (gate_up, down)]
+    d = pivot_moe_desc(n, top_k, PIVOT_F32 if router.dtype == np.float32 else PIVOT_F16,
+                       flags | (PIVOT_MOE_RENORMALISE if renormalise else 0), norm_eps)
+    out = C.c_void_p()
+    _check(lib().pivot_moe_plan(C.byref(d), handles[0], handles[1], _np_ptr(router), _np_ptr(router_bias), _np_ptr(norm_weight),
+                                C.byref(out)))
+    return out
+
+
+def pivot_moe_plan_destroy(plan):
+    lib().pivot_moe_plan_destroy(plan)
+
+
+def pivot_moe_workspace_bytes(plan, tokens):
+    return int(lib().pivot_moe_workspace_bytes(plan, tokens))
+
+
+def pivot_moe_run(plan, x_ptr, ldx, y_ptr, ldy, tokens, ws_ptr, ws_bytes, stream=None, *, xtype=PIVOT_F16, res_ptr=None, ids_ptr=None,
+                  weights_ptr=None):
+    _check(lib().pivot_moe_run(plan, x_ptr, xtype, ldx, res_ptr, y_ptr, ldy, tokens, ids_ptr, weights_ptr, ws_ptr, ws_bytes, stream))
