@@ -19,7 +19,7 @@ namespace pivot {
 
 namespace {
 
-constexpr int kRouterThreads = 256;
+constexpr int kRouterThreads = 1024;
 
 template <typename T>
 __device__ __forceinline__ void router_load8(const T* p, int c, int D, bool vec, float (&v)[8]) {
@@ -39,210 +39,232 @@ __device__ __forceinline__ void router_load8(const T* p, int c, int D, bool vec,
     }
 }
 
-template <typename RT>
+// The largest of 64 lanes (no NaNs), in every lane.
+template <int CTRL>
+__device__ __forceinline__ float dpp_max(float v) {
+    return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false)));
+}
+__device__ __forceinline__ float lane_of(float v, int l) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l));
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
+    return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    v = group_sum<16>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+
+// 16 wavefronts: TP tokens (the number of tokens, to the next power of two), 16 / TP wavefronts to each for the logit of
+// expert blockIdx.x; in the last workgroup to arrive a wavefront per token for the choice.
+template <typename RT, int TP>
 __global__ void __launch_bounds__(kRouterThreads) moe_router_kernel(MoeLaunch a, int vec) {
-    __shared__ float s_red[kRouterThreads / 64][kMoeMaxTokens];
-    __shared__ float s_logit[kMoeMaxTokens][kMoeMaxExperts];
+    constexpr int S = 16 / TP;
+    __shared__ float s_red[16];
     __shared__ int   s_sel[kMoeMaxTokens][kMoeMaxTopK];
     __shared__ float s_w[kMoeMaxTokens][kMoeMaxTopK];
-    __shared__ int   s_base[kRouterThreads / 64], s_last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, e = blockIdx.x, T = a.tokens, E = a.E, K = a.top_k;
-    const RT* w = reinterpret_cast<const RT*>(a.router) + (long long)e * a.D;
-    const _Float16* x = reinterpret_cast<const _Float16*>(a.x);
-    float acc[kMoeMaxTokens] = {};
-    for (int c = tid * 8; c < a.D; c += kRouterThreads * 8) {
-        float wv[8];
-        router_load8(w, c, a.D, vec, wv);
-        #pragma unroll
-        for (int t = 0; t < kMoeMaxTokens; ++t) {
-            if (t < T) {
-                float xv[8];
-                router_load8(x + t * a.ldx, c, a.D, vec, xv);
+    __shared__ int   s_mask[kMoeMaxExperts], s_at[kMoeMaxExperts], s_base[4], s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = q_wave(), e = blockIdx.x, T = a.tokens, E = a.E, K = a.top_k;
+    {
+        const int t = wave % TP;
+        const RT* w = reinterpret_cast<const RT*>(a.router) + (long long)e * a.D;
+        const _Float16* x = reinterpret_cast<const _Float16*>(a.x) + t * a.ldx;
+        float acc = 0.f;
+        if (t < T)
+            #pragma unroll 2
+            for (int c = ((wave / TP) * 64 + lane) * 8; c < a.D; c += S * 512) {
+                float wv[8], xv[8];
+                router_load8(w, c, a.D, vec, wv);
+                router_load8(x, c, a.D, vec, xv);
                 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[t] = __builtin_fmaf(wv[i], xv[i], acc[t]);
+                for (int i = 0; i < 8; ++i) acc = __builtin_fmaf(wv[i], xv[i], acc);
             }
-        }
-    }
-    #pragma unroll
-    for (int t = 0; t < kMoeMaxTokens; ++t) {
-        if (t < T) {
-            const float s = group_sum<64>(acc[t]);
-            if (lane == 0) s_red[wave][t] = s;
-        }
+        acc = wave_sum(acc);
+        if (lane == 0) s_red[wave] = acc;
     }
     __syncthreads();
     if (tid < T) {
         float s = 0.f;
         #pragma unroll
-        for (int q = 0; q < kRouterThreads / 64; ++q) s += s_red[q][tid];
+        for (int q = 0; q < S; ++q) s += s_red[q * TP + tid];
         if (a.router_bias) s += a.router_bias[e];
         agent_store(a.logits + tid * E + e, s);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the logits are out before the arrival is counted
-    __syncthreads();
+    if (wave == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the logits are out before the arrival is counted
     if (tid == 0) {
         const int last = __hip_atomic_fetch_add(&a.route->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(E - 1);
         if (last) __hip_atomic_store(&a.route->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = last;
     }
+    if (tid < kMoeMaxExperts) s_mask[tid] = 0;
+    if (tid < kMoeMaxTokens * kMoeMaxTopK) { (&s_sel[0][0])[tid] = -1; (&s_w[0][0])[tid] = 0.f; }
     __syncthreads();
     if (!s_last) return;
 
-    // ---- the last workgroup: ranks, weights, and who uses what
-    for (int i = tid; i < T * E; i += kRouterThreads) s_logit[i / E][i % E] = agent_load(a.logits + i);
-    if (tid < kMoeMaxTokens * kMoeMaxTopK) { (&s_sel[0][0])[tid] = -1; (&s_w[0][0])[tid] = 0.f; }
-    __syncthreads();
-    const float ninf = -__builtin_inff();
-    for (int t = wave; t < T; t += kRouterThreads / 64) {
-        float v[4], m = ninf;
-        int any_nan = 0;
+    // ---- the last workgroup: who uses what
+    if (wave < T) {
+        const float ninf = -__builtin_inff();
+        const int t = wave;
+        float v[4];
+        int nan = 0;
         #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            v[q] = lane + 64 * q < E ? s_logit[t][lane + 64 * q] : ninf;
-            any_nan |= v[q] != v[q];
-            m = fmaxf(m, v[q]);
+            const int i = lane + 64 * q;
+            v[q] = i < E ? agent_load(a.logits + t * E + i) : ninf;
+            nan |= v[q] != v[q];
         }
-        any_nan = __any(any_nan);
-        #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-        int rank[4] = {};
-        if (any_nan) {                                   // the first top_k experts, with weights that are NaN
-            #pragma unroll
-            for (int q = 0; q < 4; ++q) { rank[q] = lane + 64 * q; if (rank[q] < E) v[q] = __builtin_nanf(""); }
+        if (__any(nan)) {                                // the first top_k experts, with weights that are NaN
+            if (lane < K) { s_sel[t][lane] = lane; s_w[t][lane] = __builtin_nanf(""); atomicOr(&s_mask[lane], 1 << t); }
         } else {
-            for (int j = 0; j < E; ++j) {
-                const float o = s_logit[t][j];
+            float m = 0.f, s = 0.f, all = 0.f, mine = 0.f;   // mine: lane j's weight of choice j
+            int chosen = -1, n = 0;
+            for (int j = 0; j < K; ++j) {
+                float top = wave_max(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+                if (top == ninf) break;
+                if (j == 0) {
+                    m = top;
+                    #pragma unroll
+                    for (int q = 0; q < 4; ++q) all += v[q] == ninf ? 0.f : expf(v[q] - m);
+                }
+                int at = -1;                             // the lowest index among equals
                 #pragma unroll
-                for (int q = 0; q < 4; ++q) rank[q] += (o > v[q] || (o == v[q] && j < lane + 64 * q)) ? 1 : 0;
+                for (int q = 3; q >= 0; --q) {
+                    const unsigned long long b = __ballot(v[q] == top);
+                    if (b) at = 64 * q + __builtin_ctzll(b);
+                }
+                #pragma unroll
+                for (int q = 0; q < 4; ++q) if (lane + 64 * q == at) v[q] = ninf;
+                const float p = expf(top - m);
+                s += p;
+                if (lane == j) { mine = p; chosen = at; }
+                ++n;
             }
+            if (!a.renormalise) s = wave_sum(all);
+            if (lane < n) { s_sel[t][lane] = chosen; s_w[t][lane] = mine / s; atomicOr(&s_mask[chosen], 1 << t); }
         }
-        float p[4], s = 0.f;
-        bool chosen[4];
-        #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const bool real = lane + 64 * q < E && v[q] != ninf;
-            chosen[q] = real && rank[q] < K;
-            p[q] = real ? expf(v[q] - m) : 0.f;
-            if (real && (chosen[q] || !a.renormalise)) s += p[q];
-        }
-        s = group_sum<64>(s);
-        #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (chosen[q]) { s_sel[t][rank[q]] = lane + 64 * q; s_w[t][rank[q]] = p[q] / s; }
     }
+    __syncthreads();
+    // experts in use, in ascending order
+    int mask = 0, at = 0, total = 0;
+    unsigned long long used = 0;
+    if (tid < kMoeMaxExperts) {
+        mask = s_mask[tid];
+        used = __ballot(mask != 0);
+        if (lane == 0) s_base[wave] = __popcll(used);
+    }
+    __syncthreads();
+    #pragma unroll
+    for (int q = 0; q < 4; ++q) { if (q < wave) at += s_base[q]; total += s_base[q]; }
+    at += __popcll(used & ((1ull << lane) - 1));
+    if (tid < kMoeMaxExperts) s_at[tid] = at;
+    if (mask) {
+        unsigned long long tok = 0;
+        for (int left = mask, m = 0; left; left &= left - 1, ++m) tok |= (unsigned long long)__builtin_ctz(left) << (4 * m);
+        a.route->active[at].ntok = __popc(mask);
+        a.route->active[at].mask = mask;
+        a.route->active[at].tok = tok;
+    }
+    if (tid == 0) a.route->n = total;
     __syncthreads();
     if (tid < T * K) {
-        const int t = tid / K, j = tid % K;
-        a.route->sel[t][j] = s_sel[t][j];
-        a.route->sel_w[t][j] = s_w[t][j];
-        if (a.ids) a.ids[tid] = s_sel[t][j];
-        if (a.weights) a.weights[tid] = s_w[t][j];
-    }
-    // experts in use, in ascending order: thread e counts expert e's tokens
-    int n = 0;
-    if (tid < E)
-        for (int i = 0; i < T * K; ++i) n += s_sel[i / K][i % K] == tid;
-    const unsigned long long used = __ballot(n > 0);
-    if (lane == 0) s_base[wave] = __popcll(used);
-    __syncthreads();
-    int at = __popcll(used & ((1ull << lane) - 1)), total = 0;
-    #pragma unroll
-    for (int q = 0; q < kRouterThreads / 64; ++q) { if (q < wave) at += s_base[q]; total += s_base[q]; }
-    if (tid == 0) a.route->n = total;
-    if (n > 0) {
-        a.route->expert[at] = tid;
-        a.route->ntok[at] = n;
-        int m = 0;
-        for (int t = 0; t < kMoeMaxTokens; ++t) {
-            int row = -1;
-            float share = 0.f;
-            if (t < T)
-                for (int j = 0; j < K; ++j)
-                    if (s_sel[t][j] == tid) { row = t * K + j; share = s_w[t][j]; }
-            a.route->hrow[at][t] = row;
-            a.route->share[at][t] = share;
-            if (row >= 0) a.route->tok[at][m++] = t;
+        const int t = tid / K, j = tid % K, ex = s_sel[t][j];
+        const float w = s_w[t][j];
+        a.route->sel[t][j] = ex;
+        a.route->sel_w[t][j] = w;
+        if (a.ids) a.ids[tid] = ex;
+        if (a.weights) a.weights[tid] = w;
+        if (ex >= 0) {
+            MoeActive& act = a.route->active[s_at[ex]];
+            const int m = __popc(s_mask[ex] & ((1 << t) - 1));
+            act.hrow[m] = tid;
+            act.share[t] = w;
         }
+    }
+    // the experts' layers beside them
+    constexpr int NW = sizeof(MoeExpert) / 8;
+    for (int i = tid; i < E * NW; i += kRouterThreads) {
+        const int ex = i / NW;
+        if (s_mask[ex]) reinterpret_cast<unsigned long long*>(&a.route->active[s_at[ex]].ex)[i % NW] = reinterpret_cast<const unsigned long long*>(&a.experts[ex])[i % NW];
     }
 }
 
-template <int GPK, bool ZP, int P, int W>
-__global__ void __launch_bounds__(W * 64) moe_up_kernel(MoeLaunch a, int vec) {
-    constexpr int ROW = QElem<false>::kRow;
+// gridDim.y: experts in use, at most; blockIdx.x: RS strips of a block row.  As the rows form of a layer, the rows of x
+// being the expert's tokens.
+template <int GPK, bool ZP, int RS, bool FAST, int W>
+__global__ void __launch_bounds__(W * 64, 4) moe_up_kernel(MoeLaunch a, int vec) {
+    constexpr int N = 256 * RS;
     extern __shared__ __align__(16) char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int act = blockIdx.y, strip = blockIdx.x;
-    if (act >= a.route->n) return;
-    const int e = a.route->expert[act], ntok = a.route->ntok[act], T = a.tokens;
-    const MoeExpert& ex = a.experts[e];
-    const int sb = a.bh[0] / kQStrip, br = strip / sb, bw_log2 = 31 - __clz(a.bw[0]);
-    const int kb0 = ex.kb_ptr[0][br], nkb = ex.kb_ptr[0][br + 1] - kb0;
-    const size_t unit0 = (size_t)kb0 * sb + (size_t)(strip % sb) * nkb;
-    const u32x4* codes = reinterpret_cast<const u32x4*>(ex.codes[0]); const uint16_t* scales = ex.scales[0]; const int8_t* zoff = ex.zoff[0];
-    const int32_t* pieces = ex.pieces[0] + ((size_t)kb0 << (7 - bw_log2));
-    const QSource x{a.x, a.ldx, ex.pcol, a.D, vec};
-    char* xs = smem + wave * (P * T * ROW);
-    const int nrow[1] = {min(lane & 15, ntok - 1) * ROW};
-    f32x4 acc[1][1] = {};
-    const int sp = (lane >> 4) % P, c8 = lane & 15;
-    for (int kb = wave; kb < nkb; kb += W * P) {
-        QUnit<GPK, ZP> u[P][1];
-        #pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (kb + p * W < nkb) u[p][0].load(codes, scales, zoff, unit0 + kb + p * W, lane);
-        const int skb = kb + sp * W;
-        if (skb < nkb) {
-            const int c = 8 * c8, piece0 = gload<int>(pieces + (skb << (7 - bw_log2)) + (c >> bw_log2));
-            const int col = piece0 < 0 ? a.D : piece0 + (c & ((1 << bw_log2) - 1));
-            i32x4 idx[2] = {i32x4{-1, -1, -1, -1}, i32x4{-1, -1, -1, -1}};
-            if (x.pcol && piece0 >= 0) { idx[0] = gload<i32x4>(x.pcol + col); idx[1] = gload<i32x4>(x.pcol + col + 4); }
-            for (int m = (lane >> 4) / P; m < ntok; m += 4 / P) {
-                __align__(16) _Float16 v[8];
-                q_load8<false>(x, a.route->tok[act][m], col, idx, v);
-                q_store8<false>(xs + (sp * T + m) * ROW, c8, v);
-            }
-        }
-        wave_lds_sync();
-        #pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (kb + p * W < nkb) q_multiply<false, GPK, ZP, 1, 1>(u[p], xs + p * T * ROW, nrow, lane, acc);
-        wave_lds_sync();
+    const int tid = threadIdx.x, lane = tid & 63, wave = q_wave(), T = a.tokens;
+    const MoeActive& act = a.route->active[blockIdx.y];
+    const MoeExpert& ex = act.ex;
+    const int n_act = a.route->n, ntok = act.ntok, whole = ex.whole[0];
+    const unsigned long long tok = act.tok;
+    if ((int)blockIdx.y >= n_act) return;
+    const int strip = blockIdx.x * RS, sb = a.bh[0] / kQStrip, br = strip / sb, bw_log2 = 31 - __clz(a.bw[0]);
+    const int kb0 = whole ? br * whole : ex.kb_ptr[0][br], nkb = whole ? whole : ex.kb_ptr[0][br + 1] - kb0;
+    // what the end needs is asked for now
+    const int em = tid / (8 * RS), eu = tid % (8 * RS);
+    int dst = -1, hrow = 0;
+    float bg = 0.f, bu = 0.f;
+    if (em < ntok) {
+        dst = gload<int>(ex.hdst + strip * 8 + eu);
+        hrow = act.hrow[em];
+        bg = gload<float>(ex.bias[0] + strip * 16 + 2 * eu);
+        bu = gload<float>(ex.bias[0] + strip * 16 + 2 * eu + 1);
     }
+    f32x4 acc[RS][1] = {};
+    const QWalk k{reinterpret_cast<const u32x4*>(ex.codes[0]), ex.scales[0], ex.zeros[0], whole ? nullptr : ex.pieces[0] + ((size_t)kb0 << (7 - bw_log2)),
+                  (size_t)kb0 * sb + (size_t)(strip % sb) * nkb, nkb, wave, nkb, bw_log2};
+    q_walk_rows<false, GPK, ZP, RS, FAST, W>(k, QSource{a.x, a.ldx, ex.pcol, a.D, vec}, ntok, [&](int m) { return (int)(tok >> (4 * m)) & 15; },
+                                           smem + wave * (2 * T * QElem<false>::kRow), acc);
     __syncthreads();
     float* red = reinterpret_cast<float*>(smem);
     #pragma unroll
-    for (int i = 0; i < 4; ++i) red[wave * 256 + (lane & 15) * 16 + 4 * (lane >> 4) + i] = acc[0][0][i];
-    __syncthreads();
-    if (tid < 8 * ntok) {
-        const int m = tid / 8, u = tid % 8, r = strip * 16 + 2 * u, dst = ex.hdst[strip * 8 + u];
-        float g = 0.f, v = 0.f;
+    for (int r = 0; r < RS; ++r)
         #pragma unroll
-        for (int w = 0; w < W; ++w) { g += red[w * 256 + m * 16 + 2 * u]; v += red[w * 256 + m * 16 + 2 * u + 1]; }
-        g += ex.bias[0][r];
-        v += ex.bias[0][r + 1];
+        for (int i = 0; i < 4; ++i) red[wave * N + (lane & 15) * (16 * RS) + 16 * r + 4 * (lane >> 4) + i] = acc[r][0][i];
+    __syncthreads();
+    auto finish = [&](int m, int u, int to, int row, float g, float v) {
+        #pragma unroll
+        for (int w = 0; w < W; ++w) { g += red[w * N + m * 16 * RS + 2 * u]; v += red[w * N + m * 16 * RS + 2 * u + 1]; }
         const float h = g / (1.f + expf(-g)) * v;
         const _Float16 hi = (_Float16)h;
         // what fp16 leaves of h, 2^11 times: again fp16; nothing where h is beyond the range
         const _Float16 lo = fabsf((float)hi) < __builtin_inff() ? (_Float16)((h - (float)hi) * 2048.f) : (_Float16)0.f;
-        if (dst >= 0) {
-            _Float16* out = reinterpret_cast<_Float16*>(a.h) + (size_t)a.route->hrow[act][a.route->tok[act][m]] * a.F_pad + dst;
+        if (to >= 0) {
+            _Float16* out = reinterpret_cast<_Float16*>(a.h) + (size_t)row * a.F_pad + to;
             out[0] = hi;
             out[(size_t)T * a.top_k * a.F_pad] = lo;
         }
+    };
+    if (blockIdx.x == 0)                                 // the columns that fill up the down layer's last tile
+        for (int i = tid; i < 2 * ntok * (a.F_pad - a.F); i += W * 64) {
+            const int m = i / (2 * (a.F_pad - a.F)), r = i % (2 * (a.F_pad - a.F)), plane = r & 1;
+            a.h[((size_t)plane * T * a.top_k + act.hrow[m]) * a.F_pad + a.F + r / 2] = 0;
+        }
+    if (em < ntok) finish(em, eu, dst, hrow, bg, bu);
+    for (int i = tid + W * 64; i < 8 * RS * ntok; i += W * 64) {
+        const int m = i / (8 * RS), u = i % (8 * RS);
+        finish(m, u, ex.hdst[strip * 8 + u], act.hrow[m], ex.bias[0][strip * 16 + 2 * u], ex.bias[0][strip * 16 + 2 * u + 1]);
     }
 }
 
-// An expert in use, for one strip of its down layer.
-struct DownExpert { const u32x4* codes; const uint16_t* scales; const int8_t* zoff; const int32_t* pieces; };
-
-template <int GPK, bool ZP, int P, int W>
-__global__ void __launch_bounds__(W * 64) moe_down_kernel(MoeLaunch a) {
-    static_assert(P == 2 || P == 4, "the staging takes two planes of P units with four groups of lanes");
-    constexpr int ROW = QElem<false>::kRow;
+// blockIdx.x: a strip of outputs; the units of all experts in use are one list, which the wavefronts of the strip's
+// gridDim.y workgroups take in turn, P at a time.  NT = 2: values and remainders of h are two column tiles; NT = 1 (up to 8 tokens): columns 0-7 and 8-15 of one.
+// rows that a wavefront stages: at least the values and remainders of all tokens in one unit
+template <int NT> constexpr int kDownRows = 16 * NT;
+template <int GPK, bool ZP, int NT, int W>
+__global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
+    constexpr int ROW = QElem<false>::kRow, P = 2;       // (two units a turn: the list of rows is split in two)
+    struct Down { const u32x4* codes; const uint16_t* scales; const uint8_t* zeros; const int32_t* pieces; };
     extern __shared__ __align__(16) char smem[];
-    __shared__ DownExpert s_ex[kMoeMaxActive];
-    __shared__ int s_cum[kMoeMaxActive + 1];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, T = a.tokens, n_act = a.route->n;
+    __shared__ Down s_ex[kMoeMaxActive];
+    __shared__ int s_cum[kMoeMaxActive + 1], s_mask[kMoeMaxActive];
+    __shared__ float s_share[kMoeMaxActive][kMoeMaxTokens];
+    __shared__ uint8_t s_hrow[kMoeMaxActive][kMoeMaxTokens];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = q_wave(), T = a.tokens, n_act = a.route->n, parts = gridDim.y, step = W * parts;
     const int strip = blockIdx.x, sb = a.bh[1] / kQStrip, br = strip / sb, bw_log2 = 31 - __clz(a.bw[1]);
     if (wave == 0) {                                    // block counts of the experts in use, and their running sum
         int run = 0;
@@ -250,12 +272,13 @@ __global__ void __launch_bounds__(W * 64) moe_down_kernel(MoeLaunch a) {
             const int i = base + lane;
             int nkb = 0;
             if (i < n_act) {
-                const MoeExpert& ex = a.experts[a.route->expert[i]];
-                const int kb0 = ex.kb_ptr[1][br];
-                nkb = ex.kb_ptr[1][br + 1] - kb0;
+                const MoeExpert& ex = a.route->active[i].ex;
+                const int whole = ex.whole[1], kb0 = whole ? br * whole : ex.kb_ptr[1][br];
+                nkb = whole ? whole : ex.kb_ptr[1][br + 1] - kb0;
                 const size_t unit0 = (size_t)kb0 * sb + (size_t)(strip % sb) * nkb;
-                s_ex[i] = DownExpert{reinterpret_cast<const u32x4*>(ex.codes[1]) + unit0 * 64, ex.scales[1] + unit0 * GPK * kQStrip,
-                                     ZP ? ex.zoff[1] + unit0 * GPK * kQStrip : nullptr, ex.pieces[1] + ((size_t)kb0 << (7 - bw_log2))};
+                s_ex[i] = Down{reinterpret_cast<const u32x4*>(ex.codes[1]) + unit0 * 64, ex.scales[1] + unit0 * GPK * kQStrip,
+                               ZP ? ex.zeros[1] + unit0 * GPK * kQStrip : nullptr, whole ? nullptr : ex.pieces[1] + ((size_t)kb0 << (7 - bw_log2))};
+                s_mask[i] = a.route->active[i].mask;
             }
             int s = nkb;
             #pragma unroll
@@ -264,76 +287,146 @@ __global__ void __launch_bounds__(W * 64) moe_down_kernel(MoeLaunch a) {
             run += __shfl(s, 63, 64);
         }
         if (lane == 0) s_cum[0] = 0;
+    } else {
+        for (int i = tid - 64; i < n_act * kMoeMaxTokens; i += (W - 1) * 64) {
+            const MoeActive& act = a.route->active[i / kMoeMaxTokens];
+            s_share[i / kMoeMaxTokens][i % kMoeMaxTokens] = act.share[i % kMoeMaxTokens];
+            s_hrow[i / kMoeMaxTokens][i % kMoeMaxTokens] = (uint8_t)act.hrow[i % kMoeMaxTokens];
+        }
     }
     __syncthreads();
     const int units = s_cum[n_act];
-    char* xs = smem + wave * (P * 2 * T * ROW);
-    const int n = min(lane & 15, T - 1);
-    f32x4 total = {};
+    char* xs = smem + wave * (kDownRows<NT> * ROW);
+    // this lane's column: a token, its value or (second half of a single tile) its remainder
+    const int n = NT == 1 ? (lane & 7) : (lane & 15), second = NT == 1 ? (lane >> 3) & 1 : 0;
+    f32x4 total[NT] = {};
     int cur = 0;
-    for (int u0 = wave; u0 < units; u0 += W * P) {
-        QUnit<GPK, ZP> u[P][1];
-        int act[P], kb[P];
+    // A turn: P units, their rows of h (values, then remainders, of each unit's tokens) as one list of which the first
+    // twelve are asked for ahead.  As in the rows form every load is issued whatever the sizes: past the end the last unit's.
+    constexpr int NX = 3;
+    struct Turn { QUnit<GPK, ZP> u[P][1]; u32x4 v[NX]; int act[P], kb[P], mask[P], off[P + 1]; };
+    const int c = 8 * (lane & 15), in = c & ((1 << bw_log2) - 1), slot = lane >> 4;
+    auto column = [&](int act, int kb) {                // where this lane's columns of a block begin, F and more: nowhere
+        const int32_t* pieces = s_ex[act].pieces;
+        const int piece = pieces ? gload<int>(pieces + (kb << (7 - bw_log2)) + (c >> bw_log2)) : (kb << 7) + c - in;
+        return piece < 0 ? a.F : piece + in;
+    };
+    auto values = [&](int act, int r, int ntok, int col) -> u32x4 {
+        const int plane = r >= ntok, m = r - plane * ntok;
+        const uint16_t* row = a.h + ((size_t)plane * T * a.top_k + s_hrow[act][m]) * a.F_pad;
+        u32x4 v = gload<u32x4>(row + min(col, a.F_pad - 8));           // (columns between F and F_pad hold zeros)
+        if (col >= a.F_pad) v = u32x4{};
+        return v;
+    };
+    auto fetch = [&](Turn& t, int u0) {
+        t.off[0] = 0;
         #pragma unroll
         for (int p = 0; p < P; ++p) {
-            const int g = u0 + p * W;
-            if (g < units) {
-                while (g >= s_cum[cur + 1]) ++cur;
-                act[p] = __builtin_amdgcn_readfirstlane(cur);
-                kb[p] = __builtin_amdgcn_readfirstlane(g - s_cum[cur]);
-                const DownExpert ex = s_ex[act[p]];
-                u[p][0].load(ex.codes, ex.scales, ex.zoff, kb[p], lane);
-            } else { act[p] = -1; kb[p] = 0; }
+            const int g = min(u0 + p * step, units - 1);
+            while (g >= s_cum[cur + 1]) ++cur;
+            t.act[p] = __builtin_amdgcn_readfirstlane(cur);
+            t.kb[p] = __builtin_amdgcn_readfirstlane(g - s_cum[cur]);
+            t.mask[p] = u0 + p * step < units ? __builtin_amdgcn_readfirstlane(s_mask[cur]) : 0;
+            t.off[p + 1] = t.off[p] + 2 * __popc(t.mask[p]);
         }
-        const int c = 8 * (lane & 15);
+        int act[NX], at[NX], ntok[NX], col[NX];         // this lane's row of h in each place of the list
         #pragma unroll
-        for (int q = 0; q < P / 2; ++q) {
-            // lane groups 0 and 1: the two units of this turn, plane 0; groups 2 and 3: plane 1
-            const int sel = (lane >> 4) & 1, plane = lane >> 5, p = 2 * q + sel;
-            const int sa = sel ? act[2 * q + 1] : act[2 * q], skb = sel ? kb[2 * q + 1] : kb[2 * q];
-            if (sa >= 0) {
-                const int piece0 = gload<int>(s_ex[sa].pieces + (skb << (7 - bw_log2)) + (c >> bw_log2));
-                const int col = piece0 < 0 ? a.F : piece0 + (c & ((1 << bw_log2) - 1));
-                const QSource h{a.h + (size_t)plane * T * a.top_k * a.F_pad, a.F_pad, nullptr, a.F, 1};
-                const int ntok = a.route->ntok[sa];
-                const i32x4 none[2] = {};
-                for (int m = 0; m < ntok; ++m) {
-                    const int t = a.route->tok[sa][m];
-                    __align__(16) _Float16 v[8];
-                    q_load8<false>(h, a.route->hrow[sa][t], col, none, v);
-                    q_store8<false>(xs + ((p * 2 + plane) * T + t) * ROW, lane & 15, v);
-                }
-            }
+        for (int q = 0; q < NX; ++q) {
+            const int i = max(0, min(slot + 4 * q, t.off[P] - 1));
+            const bool first = i < t.off[1];
+            act[q] = first ? t.act[0] : t.act[1];
+            at[q] = first ? i : i - t.off[1];
+            ntok[q] = __popc(first ? t.mask[0] : t.mask[1]);
+            col[q] = column(act[q], first ? t.kb[0] : t.kb[1]);
         }
-        wave_lds_sync();
+        #pragma unroll
+        for (int p = 0; p < P; ++p) t.u[p][0].load(s_ex[t.act[p]].codes, s_ex[t.act[p]].scales, s_ex[t.act[p]].zeros, t.kb[p], lane);
+        #pragma unroll
+        for (int q = 0; q < NX; ++q) t.v[q] = values(act[q], at[q], ntok[q], col[q]);
+    };
+    auto multiply_unit = [&](const Turn& t, int p, int at) {
+        const int mask = t.mask[p], ntok = __popc(mask);
+        const bool mine = (mask >> n) & 1;
+        const int m = mine ? __popc(mask & ((1 << n) - 1)) : 0;
+        int nrow[NT];
+        #pragma unroll
+        for (int q = 0; q < NT; ++q) nrow[q] = (at + m + (q + second) * ntok) * ROW;
+        f32x4 part[1][NT] = {};
+        const QRows<false, NT> x{xs, nrow, lane};
+        q_multiply<false, GPK, ZP, NT, 1>(t.u[p], x, part);
+        // tokens that do not use the expert: what their column held is dropped
+        const float share = s_share[t.act[p]][n];
+        #pragma unroll
+        for (int q = 0; q < NT; ++q)
+            #pragma unroll
+            for (int i = 0; i < 4; ++i) total[q][i] = mine ? __builtin_fmaf(share, part[0][q][i], total[q][i]) : total[q][i];
+    };
+    auto multiply = [&](const Turn& t) {
+        const bool ahead = t.off[P] <= 4 * NX;
+        if (ahead)
+            #pragma unroll
+            for (int q = 0; q < NX; ++q) if (slot + 4 * q < t.off[P]) q_store8<false>(xs + (slot + 4 * q) * ROW, lane & 15, t.v[q]);
         #pragma unroll
         for (int p = 0; p < P; ++p)
-            if (act[p] >= 0) {
-                const int nrow[2] = {(p * 2 * T + n) * ROW, ((p * 2 + 1) * T + n) * ROW};
-                f32x4 part[1][2] = {};
-                q_multiply<false, GPK, ZP, 2, 1>(u[p], xs, nrow, lane, part);
-                // tokens that do not use the expert: whatever their column held is dropped
-                const bool mine = a.route->hrow[act[p]][n] >= 0;
-                const float share = a.route->share[act[p]][n];
-                #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float s = __builtin_fmaf(part[0][1][i], 1.f / 2048.f, part[0][0][i]);
-                    total[i] = mine ? __builtin_fmaf(share, s, total[i]) : total[i];
+            if (t.mask[p]) {
+                if (!ahead) {                           // many tokens on few experts: a unit's rows at a time
+                    const int ntok = __popc(t.mask[p]), col = column(t.act[p], t.kb[p]);
+                    for (int r = slot; r < 2 * ntok; r += 4) q_store8<false>(xs + r * ROW, lane & 15, values(t.act[p], r, ntok, col));
                 }
+                wave_lds_sync();
+                multiply_unit(t, p, ahead ? t.off[p] : 0);
+                __builtin_amdgcn_sched_barrier(0);
+                wave_lds_sync();
             }
-        wave_lds_sync();
+    };
+    int u0 = wave + W * blockIdx.y;
+    if (u0 < units) {
+        Turn t0, t1;
+        fetch(t0, u0);
+        while (true) {
+            fetch(t1, u0 + step * P);
+            multiply(t0);
+            u0 += step * P;
+            if (u0 >= units) break;
+            fetch(t0, u0 + step * P);
+            multiply(t1);
+            u0 += step * P;
+            if (u0 >= units) break;
+        }
     }
     __syncthreads();
-    float* red = reinterpret_cast<float*>(smem);
+    float* red = reinterpret_cast<float*>(smem);        // [wave][tile][column][row]
     #pragma unroll
-    for (int i = 0; i < 4; ++i) red[wave * 256 + (lane & 15) * 16 + 4 * (lane >> 4) + i] = total[i];
+    for (int t = 0; t < NT; ++t)
+        #pragma unroll
+        for (int i = 0; i < 4; ++i) red[(wave * NT + t) * 256 + (lane & 15) * 16 + 4 * (lane >> 4) + i] = total[t][i];
     __syncthreads();
+    auto sum_of = [&](int i) {
+        float s = 0.f, lo = 0.f;
+        #pragma unroll
+        for (int w = 0; w < W; ++w) { s += red[w * NT * 256 + i]; lo += red[w * NT * 256 + i + (NT == 1 ? 128 : 256)]; }
+        return __builtin_fmaf(lo, 1.f / 2048.f, s);
+    };
+    float* mine = a.partials + (size_t)strip * parts * 16 * T;
+    if (parts > 1) {                                    // handed over as the pieces of a block row of a layer are
+        for (int i = tid; i < 16 * T; i += W * 64) agent_store(mine + blockIdx.y * 16 * T + i, sum_of(i));
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) {
+            uint32_t* tk = a.tickets + (size_t)strip * kQTicketStride;
+            const int last = __hip_atomic_fetch_add(tk, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
+            if (last) __hip_atomic_store(tk, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = last;
+        }
+        __syncthreads();
+        if (!s_last) return;
+    }
     for (int i = tid; i < 16 * T; i += W * 64) {
         const int t = i / 16, r = strip * 16 + i % 16, dst = a.prow_down[r];
         if (dst < 0) continue;
         float s = 0.f;
-        #pragma unroll
-        for (int w = 0; w < W; ++w) s += red[w * 256 + i];
+        if (parts > 1) { for (int q = 0; q < parts; ++q) s += agent_load(mine + q * 16 * T + i); }
+        else s = sum_of(i);
         for (int j = 0; j < a.top_k; ++j) {
             const int e = a.route->sel[t][j];
             if (e >= 0) s = __builtin_fmaf(a.route->sel_w[t][j], a.experts[e].bias[1][r], s);
@@ -357,41 +450,60 @@ int reserve(const void* k, size_t smem) {
     return PIVOT_OK;
 }
 
-template <int GPK, bool ZP, int P>
+template <int GPK, bool ZP>
 int up_go(const MoeLaunch& L, int vec) {
-    constexpr int W = 8;
-    auto k = moe_up_kernel<GPK, ZP, P, W>;
-    const size_t smem = std::max((size_t)W * P * L.tokens * QElem<false>::kRow, (size_t)W * 1024);
-    int rc = reserve(reinterpret_cast<const void*>(k), smem);
-    if (rc != PIVOT_OK) return rc;
-    hipLaunchKernelGGL(k, dim3(L.nstrips[0], std::min(L.E, L.tokens * L.top_k)), dim3(W * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L, vec);
-    return launched();
+    auto go = [&](auto k, int rs, int w) {
+        const size_t smem = std::max((size_t)w * 2 * L.tokens * QElem<false>::kRow, (size_t)w * 1024 * rs);
+        const int rc = reserve(reinterpret_cast<const void*>(k), smem);
+        if (rc != PIVOT_OK) return rc;
+        hipLaunchKernelGGL(k, dim3(L.nstrips[0] / rs, std::min(L.E, L.tokens * L.top_k)), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L, vec);
+        return launched();
+    };
+    const int most = std::min(2, L.bh[0] / kQStrip), active = std::min(L.E, L.tokens * L.top_k);
+    int rs = 1;
+    while (rs < most && L.nstrips[0] * active / (2 * rs) >= 512) rs *= 2;
+    if (!(L.gather == 0 && vec && L.D % 8 == 0)) return go(moe_up_kernel<GPK, ZP, 1, false, 4>, 1, 4);
+    return rs == 1 ? go(moe_up_kernel<GPK, ZP, 1, true, 4>, 1, 4) : go(moe_up_kernel<GPK, ZP, 2, true, 4>, 2, 4);
 }
 
-template <int GPK, bool ZP, int P>
+template <int GPK, bool ZP>
 int down_go(const MoeLaunch& L, int) {
-    constexpr int W = 8;
-    auto k = moe_down_kernel<GPK, ZP, P, W>;
-    const size_t smem = std::max((size_t)W * P * 2 * L.tokens * QElem<false>::kRow, (size_t)W * 1024);
-    int rc = reserve(reinterpret_cast<const void*>(k), smem);
-    if (rc != PIVOT_OK) return rc;
-    hipLaunchKernelGGL(k, dim3(L.nstrips[1]), dim3(W * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L);
-    return launched();
+    auto go = [&](auto k, int w, int rows) {
+        // Workgroups of a strip: until there are two for every compute unit, with at least two units to a wavefront.
+        const int units = L.mean_kb[1] * std::min(L.E, L.tokens * L.top_k);
+        int parts = 1;
+        while (parts < kMoeMaxParts && L.nstrips[1] * parts < 1024 && units >= 4 * w * parts) parts *= 2;
+        const size_t smem = (size_t)w * rows * QElem<false>::kRow;      // more than the sums'
+        const int rc = reserve(reinterpret_cast<const void*>(k), smem);
+        if (rc != PIVOT_OK) return rc;
+        hipLaunchKernelGGL(k, dim3(L.nstrips[1], parts), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L);
+        return launched();
+    };
+    return L.tokens <= 8 ? go(moe_down_kernel<GPK, ZP, 1, 4>, 4, kDownRows<1>) : go(moe_down_kernel<GPK, ZP, 2, 4>, 4, kDownRows<2>);
 }
 
-#define PIVOT_MOE_PICK(go, which)                                                                       \
-    (L.zeros[which] ? (L.gpk[which] == 1 ? PIVOT_MOE_P(go, 1, true) : L.gpk[which] == 2 ? PIVOT_MOE_P(go, 2, true) : PIVOT_MOE_P(go, 4, true)) \
-                    : (L.gpk[which] == 1 ? PIVOT_MOE_P(go, 1, false) : L.gpk[which] == 2 ? PIVOT_MOE_P(go, 2, false) : PIVOT_MOE_P(go, 4, false)))
-#define PIVOT_MOE_P(go, gpk, zp) (L.tokens <= 4 ? go<gpk, zp, 4>(L, vec) : go<gpk, zp, 2>(L, vec))
+template <typename RT>
+int router_go(const MoeLaunch& L, int vec) {
+    auto go = [&](auto k) {
+        hipLaunchKernelGGL(k, dim3(L.E), dim3(kRouterThreads), 0, reinterpret_cast<hipStream_t>(L.stream), L, vec);
+        return launched();
+    };
+    if (L.tokens == 1) return go(moe_router_kernel<RT, 1>);
+    if (L.tokens == 2) return go(moe_router_kernel<RT, 2>);
+    if (L.tokens <= 4) return go(moe_router_kernel<RT, 4>);
+    if (L.tokens <= 8) return go(moe_router_kernel<RT, 8>);
+    return go(moe_router_kernel<RT, 16>);
+}
+
+#define PIVOT_MOE_PICK(go, which)                                                                                          \
+    (L.zeros[which] ? (L.gpk[which] == 1 ? go<1, true>(L, vec) : L.gpk[which] == 2 ? go<2, true>(L, vec) : go<4, true>(L, vec)) \
+                    : (L.gpk[which] == 1 ? go<1, false>(L, vec) : L.gpk[which] == 2 ? go<2, false>(L, vec) : go<4, false>(L, vec)))
 
 }  // namespace
 
 int launch_moe(const MoeLaunch& L) {
-    hipStream_t st = reinterpret_cast<hipStream_t>(L.stream);
     const int vec = reinterpret_cast<uintptr_t>(L.x) % 16 == 0 && (L.ldx % 8 == 0 || L.tokens == 1), rvec = vec && L.D % 8 == 0;
-    if (L.router_type == PIVOT_F16) hipLaunchKernelGGL(moe_router_kernel<_Float16>, dim3(L.E), dim3(kRouterThreads), 0, st, L, rvec);
-    else                            hipLaunchKernelGGL(moe_router_kernel<float>, dim3(L.E), dim3(kRouterThreads), 0, st, L, rvec);
-    int rc = launched();
+    int rc = L.router_type == PIVOT_F16 ? router_go<_Float16>(L, rvec) : router_go<float>(L, rvec);
     if (rc != PIVOT_OK) return rc;
     rc = PIVOT_MOE_PICK(up_go, 0);
     if (rc != PIVOT_OK) return rc;

@@ -9,69 +9,39 @@
 namespace pivot {
 
 struct QfcArgs {
-    const u32x4* codes; const uint16_t* scales; const int8_t* zoff; const int32_t* chunks; const int32_t* kb_ptr; const int32_t* pieces;
+    const u32x4* codes; const uint16_t* scales; const uint8_t* zeros; const int32_t* chunks; const int32_t* kb_ptr; const int32_t* pieces;
     const int32_t* prow; const float* bias; const float* xscale;
-    QSource x;
+    QSource x;              // rows form: the rows; fragment form: x.x alone
     float* y; long long ldy; float* partials; uint32_t* tickets;
-    int bh, bw_log2, batch, act;
+    int bh, bw_log2, batch, act, zero_chunk, whole;   // whole > 0: every tile is kept, so many blocks in each block row
 };
 
-// One work item: RS strips of a block row times a piece of its columns, NT * 16 batch columns; blockIdx.x = piece *
-// (strips / RS) + strip group.  Wavefront w takes the blocks w, w + W, ... of the piece, P at a time: their codes and
-// their columns of x are requested together, then multiplied.  The wavefronts' sums meet in LDS.
-template <bool Q8, int GPK, bool ZP, int NT, int RS, int P, int W>
-__global__ void __launch_bounds__(W * 64) qfc_kernel(QfcArgs a) {
-    constexpr int ROW = QElem<Q8>::kRow, N = 16 * RS * 16 * NT;
-    extern __shared__ __align__(16) char smem[];
-    __shared__ int s_last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int groups = a.bh / (kQStrip * RS);
-    const int piece = blockIdx.x / groups, sg = blockIdx.x % groups;
-    const int32_t* ch = a.chunks + 8 * piece;
-    const int br = ch[0], kb0 = ch[1], kb1 = ch[2], first = ch[3], parts = ch[4], slot = ch[5];
-    const int rowkb = a.kb_ptr[br], nkb = a.kb_ptr[br + 1] - rowkb;
-    // units of a block row: strip-major
-    const size_t unit0 = (size_t)rowkb * (a.bh / kQStrip) + (size_t)(sg * RS) * nkb - rowkb;
-    char* xs = smem + wave * (P * a.batch * ROW);
-    int nrow[NT];
-    #pragma unroll
-    for (int t = 0; t < NT; ++t) nrow[t] = min(16 * t + (lane & 15), a.batch - 1) * ROW;
-
-    f32x4 acc[RS][NT] = {};
-    const int sp = (lane >> 4) % P, c8 = lane & 15;
-    for (int kb = kb0 + wave; kb < kb1; kb += W * P) {
-        QUnit<GPK, ZP> u[P][RS];
-        #pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (kb + p * W < kb1)
-                #pragma unroll
-                for (int r = 0; r < RS; ++r) u[p][r].load(a.codes, a.scales, a.zoff, unit0 + (size_t)r * nkb + kb + p * W, lane);
-        // staging: sixteen lanes take the columns of a unit, eight each
-        const int skb = kb + sp * W;
-        if (skb < kb1) {
-            const int c = 8 * c8, piece0 = a.pieces[(skb << (7 - a.bw_log2)) + (c >> a.bw_log2)];
-            const int col = piece0 < 0 ? a.x.K : piece0 + (c & ((1 << a.bw_log2) - 1));
-            i32x4 idx[2] = {};
-            if (a.x.pcol) {
-                if (piece0 >= 0) { idx[0] = *reinterpret_cast<const i32x4*>(a.x.pcol + col); idx[1] = *reinterpret_cast<const i32x4*>(a.x.pcol + col + 4); }
-                else { idx[0] = i32x4{-1, -1, -1, -1}; idx[1] = idx[0]; }
-            }
-            for (int n = (lane >> 4) / P; n < a.batch; n += 4 / P) {
-                __align__(16) typename QElem<Q8>::type v[8];
-                q_load8<Q8>(a.x, n, col, idx, v);
-                q_store8<Q8>(xs + (sp * a.batch + n) * ROW, c8, v);
-            }
-        }
-        wave_lds_sync();
-        #pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (kb + p * W < kb1) q_multiply<Q8, GPK, ZP, NT, RS>(u[p], xs + p * a.batch * ROW, nrow, lane, acc);
-        wave_lds_sync();
+// A work item: RS strips of a block row times a piece of its columns; blockIdx.x = piece * (strips / RS) + strip group.
+template <int RS>
+struct QfcItem {
+    int br, sg, kb0, kb1, first, parts, slot, rowkb, nkb;     // blocks kb0..kb1 are numbered from the row's first
+    size_t unit0;           // unit of block kb and strip r of the item: unit0 + r * nkb + kb
+    __device__ __forceinline__ explicit QfcItem(const QfcArgs& a) {
+        const int groups = a.bh / (kQStrip * RS), piece = blockIdx.x / groups;
+        sg = blockIdx.x % groups;
+        const int32_t* ch = a.chunks + 8 * piece;
+        br = ch[0]; kb0 = ch[1]; kb1 = ch[2]; first = ch[3]; parts = ch[4]; slot = ch[5];
+        rowkb = a.whole ? br * a.whole : a.kb_ptr[br];
+        nkb = a.whole ? a.whole : a.kb_ptr[br + 1] - rowkb;
+        unit0 = (size_t)rowkb * (a.bh / kQStrip) + (size_t)(sg * RS) * nkb;      // units of a block row: strip-major
+        kb0 -= rowkb;
+        kb1 -= rowkb;
     }
+};
 
-    // sums of the wavefronts: red[wave][row][batch column]
+// Sums of the wavefronts, through LDS (W * 16 RS * 16 NT floats at `red`); pieces of a row through memory; bias,
+// activation and the scatter through prow.
+template <bool Q8, bool ZP, int NT, int RS, int W>
+__device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& it, const f32x4 (&acc)[RS][NT], float* red) {
+    constexpr int N = 16 * RS * 16 * NT;
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = q_wave();
     __syncthreads();
-    float* red = reinterpret_cast<float*>(smem);
     #pragma unroll
     for (int r = 0; r < RS; ++r)
         #pragma unroll
@@ -81,21 +51,21 @@ __global__ void __launch_bounds__(W * 64) qfc_kernel(QfcArgs a) {
                 red[wave * N + (16 * t + (lane & 15)) * (16 * RS) + 16 * r + 4 * (lane >> 4) + i] = acc[r][t][i];
     __syncthreads();
     const int n_out = 16 * RS * a.batch;
-    const size_t strip_off = (size_t)sg * n_out, slot_len = (size_t)a.bh * a.batch;
-    if (parts > 1) {
+    const size_t strip_off = (size_t)it.sg * n_out, slot_len = (size_t)a.bh * a.batch;
+    if (it.parts > 1) {
         for (int e = tid; e < n_out; e += W * 64) {
             float s = 0.f;
             #pragma unroll
             for (int w = 0; w < W; ++w) s += red[w * N + e];
-            agent_store(a.partials + slot * slot_len + strip_off + e, s);
+            agent_store(a.partials + it.slot * slot_len + strip_off + e, s);
         }
         // Every store of this workgroup is complete before its arrival is counted; the partial sums bypass the caches,
         // so nothing is written back or invalidated.
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (tid == 0) {
-            uint32_t* tk = a.tickets + ((size_t)br * (a.bh / kQStrip) + sg * RS) * kQTicketStride;
-            const int last = __hip_atomic_fetch_add(tk, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(parts - 1);
+            uint32_t* tk = a.tickets + ((size_t)it.br * (a.bh / kQStrip) + it.sg * RS) * kQTicketStride;
+            const int last = __hip_atomic_fetch_add(tk, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(it.parts - 1);
             if (last) __hip_atomic_store(tk, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             s_last = last;
         }
@@ -103,37 +73,98 @@ __global__ void __launch_bounds__(W * 64) qfc_kernel(QfcArgs a) {
         if (!s_last) return;
     }
     for (int e = tid; e < n_out; e += W * 64) {
-        const int row = br * a.bh + sg * 16 * RS + e % (16 * RS), n = e / (16 * RS), dst = a.prow[row];
+        const int row = it.br * a.bh + it.sg * 16 * RS + e % (16 * RS), n = e / (16 * RS), dst = a.prow[row];
         float s = 0.f;
-        if (parts > 1) {
-            for (int q = 0; q < parts; ++q) s += agent_load(a.partials + (first + q) * slot_len + strip_off + e);
+        if (it.parts > 1) {
+            for (int q = 0; q < it.parts; ++q) s += agent_load(a.partials + (it.first + q) * slot_len + strip_off + e);
         } else {
             #pragma unroll
             for (int w = 0; w < W; ++w) s += red[w * N + e];
         }
-        if (Q8) s *= 0.0625f * a.xscale[n];
+        if (Q8) s *= kQ8Factor<ZP> * a.xscale[n];
         if (dst >= 0) a.y[n * a.ldy + dst] = apply_act(s + a.bias[row], a.act);
     }
 }
 
-// Batch columns, strips per wavefront, blocks in flight per wavefront and wavefronts of the form a call takes.
-struct QfcForm { int nt, rs, p, w; };
-
-inline QfcForm qfc_form(const QfcHost& h, int batch) {
-    const int rs2 = h.d.bh >= 32 ? 2 : 1;
-    if (batch <= 4) return {1, 1, 4, 8};
-    if (batch <= 16) return {1, 1, 2, 8};
-    if (batch <= 32) return {2, rs2, 1, 8};
-    return {4, rs2, 1, 4};
+// Rows form, up to 16 batch rows: wavefront w takes the blocks w, w + W, ... of the item.
+template <bool Q8, int GPK, bool ZP, int RS, bool FAST, int W>
+__global__ void __launch_bounds__(W * 64, 4) qfc_rows_kernel(QfcArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    const int wave = q_wave();
+    const QfcItem<RS> it(a);
+    f32x4 acc[RS][1] = {};
+    const QWalk k{a.codes, a.scales, a.zeros, a.whole ? nullptr : a.pieces + ((size_t)it.rowkb << (7 - a.bw_log2)), it.unit0, it.nkb, it.kb0 + wave, it.kb1, a.bw_log2};
+    q_walk_rows<Q8, GPK, ZP, RS, FAST, W>(k, a.x, a.batch, [](int n) { return n; }, smem + wave * (2 * a.batch * QElem<Q8>::kRow), acc);
+    qfc_finish<Q8, ZP, 1, RS, W>(a, it, acc, reinterpret_cast<float*>(smem));
 }
+
+// Fragment form: x lies in memory as the matrix instructions read it (qfc_gather_kernel), NT * 16 batch columns.
+template <bool Q8, int GPK, bool ZP, int NT, int RS, int W>
+__global__ void __launch_bounds__(W * 64) qfc_frag_kernel(QfcArgs a) {
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 63, wave = q_wave();
+    const QfcItem<RS> it(a);
+    f32x4 acc[RS][NT] = {};
+    int at[NT];                                           // this lane's place in a chunk
+    #pragma unroll
+    for (int t = 0; t < NT; ++t) at[t] = (min(16 * t + (lane & 15), a.batch - 1) * 32 + 8 * (lane >> 4)) * QElem<Q8>::kBytes;
+    const int32_t* pieces = a.pieces + ((size_t)it.rowkb << (7 - a.bw_log2));
+    constexpr bool AHEAD = NT == 1;                       // more column tiles of x do not fit beside those in use
+    struct Turn { QUnit<GPK, ZP> u[RS]; };
+    struct Chunks { int c[4]; };
+    auto chunks_of = [&](int kb) {                        // the chunk of x under each 32 columns of a block
+        Chunks r;
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = 32 * j, in = c & ((1 << a.bw_log2) - 1), b = min(kb, it.kb1 - 1);
+            const int piece = a.whole ? (b << 7) + c - in : pieces[(b << (7 - a.bw_log2)) + (c >> a.bw_log2)];
+            r.c[j] = piece < 0 ? a.zero_chunk : min(a.zero_chunk, (piece + in) >> 5);
+        }
+        return r;
+    };
+    auto fetch = [&](Turn& t, int kb) {
+        #pragma unroll
+        for (int r = 0; r < RS; ++r) t.u[r].load(a.codes, a.scales, a.zeros, it.unit0 + (size_t)r * it.nkb + min(kb, it.kb1 - 1), lane);
+    };
+    auto fetch_x = [&](QFrag<Q8, NT>& x, const Chunks& ch) {
+        #pragma unroll
+        for (int j = 0; j < 4; ++j) x.load(reinterpret_cast<const char*>(a.x.x) + (size_t)ch.c[j] * a.batch * 32 * QElem<Q8>::kBytes, at, j);
+    };
+    // While a block is multiplied, the next one is on its way.  As in the rows form, no load depends on the sizes.
+    const int kb0 = it.kb0 + wave;
+    if (kb0 < it.kb1) {
+        Turn t0, t1;
+        QFrag<Q8, NT> x0, x1;
+        Chunks c = chunks_of(kb0), d = chunks_of(kb0 + W);
+        fetch(t0, kb0);
+        if (AHEAD) fetch_x(x0, c);
+        for (int kb = kb0;;) {
+            if (AHEAD) { c = chunks_of(kb + 2 * W); fetch_x(x1, d); } else { fetch_x(x0, c); c = chunks_of(kb + 2 * W); }
+            fetch(t1, kb + W);
+            q_multiply<Q8, GPK, ZP, NT, RS>(t0.u, x0, acc);
+            kb += W;
+            if (kb >= it.kb1) break;
+            if (AHEAD) { d = chunks_of(kb + 2 * W); fetch_x(x0, c); } else { fetch_x(x0, d); d = chunks_of(kb + 2 * W); }
+            fetch(t0, kb + W);
+            q_multiply<Q8, GPK, ZP, NT, RS>(t1.u, AHEAD ? x1 : x0, acc);
+            kb += W;
+            if (kb >= it.kb1) break;
+        }
+    }
+    qfc_finish<Q8, ZP, NT, RS, W>(a, it, acc, reinterpret_cast<float*>(smem));
+}
+
+// The form a call takes: rows (frag = 0) or fragment, column tiles, strips per item, rows form: whether x is read as
+// it lies, wavefronts.
+struct QfcForm { int frag, nt, rs, fast, w; };
 
 inline size_t qfc_smem(const QfcForm& f, int batch, int row) {
-    return std::max((size_t)f.w * f.p * batch * row, (size_t)f.w * 16 * f.rs * 16 * f.nt * 4);
+    const size_t red = (size_t)f.w * 16 * f.rs * 16 * f.nt * 4;
+    return f.frag ? red : std::max((size_t)f.w * 2 * batch * row, red);
 }
 
-template <bool Q8, int GPK, bool ZP, int NT, int RS, int P, int W>
-inline int qfc_go(const QfcArgs& a, int grid, size_t smem, void* stream) {
-    auto k = qfc_kernel<Q8, GPK, ZP, NT, RS, P, W>;
+template <typename K>
+inline int qfc_go(K k, const QfcArgs& a, int grid, int w, size_t smem, void* stream) {
     if (smem > 64 * 1024) {
         // asked for on every call: the attribute belongs to the device that is current
         if (hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess) {
@@ -142,7 +173,7 @@ inline int qfc_go(const QfcArgs& a, int grid, size_t smem, void* stream) {
             return PIVOT_E_HIP;
         }
     }
-    hipLaunchKernelGGL(k, dim3(grid), dim3(W * 64), smem, reinterpret_cast<hipStream_t>(stream), a);
+    hipLaunchKernelGGL(k, dim3(grid), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(stream), a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
     return PIVOT_OK;
@@ -150,9 +181,17 @@ inline int qfc_go(const QfcArgs& a, int grid, size_t smem, void* stream) {
 
 template <bool Q8, int GPK, bool ZP>
 inline int qfc_pick(const QfcForm& f, const QfcArgs& a, int grid, size_t smem, void* stream) {
-    if (f.nt == 1) return f.p == 4 ? qfc_go<Q8, GPK, ZP, 1, 1, 4, 8>(a, grid, smem, stream) : qfc_go<Q8, GPK, ZP, 1, 1, 2, 8>(a, grid, smem, stream);
-    if (f.nt == 2) return f.rs == 2 ? qfc_go<Q8, GPK, ZP, 2, 2, 1, 8>(a, grid, smem, stream) : qfc_go<Q8, GPK, ZP, 2, 1, 1, 8>(a, grid, smem, stream);
-    return f.rs == 2 ? qfc_go<Q8, GPK, ZP, 4, 2, 1, 4>(a, grid, smem, stream) : qfc_go<Q8, GPK, ZP, 4, 1, 1, 4>(a, grid, smem, stream);
+    auto go = [&](auto k) { return qfc_go(k, a, grid, f.w, smem, stream); };
+    if (!f.frag) {
+        if (!f.fast) return go(qfc_rows_kernel<Q8, GPK, ZP, 1, false, 8>);
+        return f.rs == 1 ? go(qfc_rows_kernel<Q8, GPK, ZP, 1, true, 8>) : go(qfc_rows_kernel<Q8, GPK, ZP, 2, true, 8>);
+    }
+    if (f.nt == 1) {
+        if (f.rs == 1) return go(qfc_frag_kernel<Q8, GPK, ZP, 1, 1, 8>);
+        return go(qfc_frag_kernel<Q8, GPK, ZP, 1, 2, 8>);
+    }
+    if (f.nt == 2) return f.rs == 1 ? go(qfc_frag_kernel<Q8, GPK, ZP, 2, 1, 8>) : go(qfc_frag_kernel<Q8, GPK, ZP, 2, 2, 8>);
+    return f.rs == 1 ? go(qfc_frag_kernel<Q8, GPK, ZP, 4, 1, 8>) : go(qfc_frag_kernel<Q8, GPK, ZP, 4, 2, 8>);
 }
 
 template <bool Q8>

@@ -36,7 +36,7 @@ struct QfcHost {
     pivot_qfc_desc d{};
     int nbr = 0, nbc = 0, M_pad = 0, K_pad = 0, T = 0, KB = 0, nchunks = 0, chunk_blocks = 0, max_parts = 1, max_kb = 0;
     int gpk = 1;                        // scale groups per unit (1, 2, 4)
-    bool has_zeros = false, identity_cols = false;
+    bool has_zeros = false, identity_cols = false, whole = false;   // whole: every tile is kept
     std::vector<int32_t> row_ptr, col_idx;
     std::vector<int32_t> kb_ptr;        // [nbr+1] blocks of 128 kept columns before block row i
     std::vector<int32_t> pieces;        // [KB * 128 / bw] first block-space column of each bw columns, -1 = none
@@ -50,8 +50,8 @@ struct QfcHost {
 struct QfcDev {
     char* base = nullptr;
     void*  codes = nullptr;             // [units][64 lanes] 16 bytes; units of block row i: strip-major
-    uint16_t* scales = nullptr;         // [units][gpk][16] fp16
-    int8_t* zoff = nullptr;             // [units][gpk][16] zero point - 8, or NULL
+    uint16_t* scales = nullptr;         // [units][4 quarters of the strip][gpk][4 rows] fp16
+    uint8_t* zeros = nullptr;           // [units][16 rows][gpk], or NULL
     int32_t* kb_ptr = nullptr;
     int32_t* pieces = nullptr;
     int32_t* chunks = nullptr;
@@ -71,11 +71,12 @@ struct QfcLaunch {
     const QfcHost* h; const QfcDev* d;
     const void* x; int xtype; int64_t ldx; const float* xscale; int block_order;
     float* y; int64_t ldy; int batch;
-    float* partials; uint32_t* tickets;
+    float* partials; uint32_t* tickets; void* xcopy;
     void* stream;
 };
 size_t qfc_ticket_bytes(const QfcHost& h);
 size_t qfc_partial_bytes(const QfcHost& h, int batch);
+size_t qfc_copy_bytes(const QfcHost& h, int batch);
 int    launch_qfc(const QfcLaunch& L, std::string* describe = nullptr);
 
 struct NormLaunch {
@@ -88,29 +89,38 @@ int launch_norm(const NormLaunch& L);
 // ---- mixture of experts
 constexpr int kMoeMaxTokens = 16, kMoeMaxExperts = 256, kMoeMaxTopK = 8;
 constexpr int kMoeMaxActive = kMoeMaxTokens * kMoeMaxTopK;
+constexpr int kMoeMaxParts = 8;         // workgroups of a strip of the down layers
 
-// One expert as the kernels see it: two layers, and where a unit's activation goes in the down layer's input.
+// One expert as the kernels see it: its two layers (0 gate/up, 1 down), and where a unit's activation goes in the down
+// layer's input.  whole > 0: every tile is kept, `whole` blocks in each block row, so that neither the blocks of a row nor
+// their columns have to be looked up.
 struct MoeExpert {
-    const void* codes[2]; const uint16_t* scales[2]; const int8_t* zoff[2]; const int32_t* kb_ptr[2]; const int32_t* pieces[2];
-    const int32_t* pcol; const int32_t* hdst; const float* bias[2];
+    const void* codes[2]; const uint16_t* scales[2]; const uint8_t* zeros[2]; const int32_t* kb_ptr[2]; const int32_t* pieces[2];
+    const int32_t* pcol; const int32_t* hdst; const float* bias[2]; int32_t whole[2];
 };
-// What the router leaves for the two expert kernels.  Experts in use are numbered 0..n-1 in ascending order.
+// What the router leaves for the two expert kernels.  Experts in use are numbered 0..n-1 in ascending order; the entry of
+// one holds its layers too, which saves the kernels behind a trip.
+struct MoeActive {
+    MoeExpert ex;
+    int32_t ntok, mask;                                   // its tokens: how many, a bit each,
+    uint64_t tok;                                         // and four bits each, ascending
+    int32_t hrow[kMoeMaxTokens];                          // their rows of h
+    float   share[kMoeMaxTokens];                         // the expert's weight, by token
+};
 struct MoeRoute {
-    uint32_t ticket; int32_t n; int32_t pad[62];
-    int32_t expert[kMoeMaxActive];
-    int32_t ntok[kMoeMaxActive];                          // tokens of the expert
-    int32_t tok[kMoeMaxActive][kMoeMaxTokens];            // which, ascending
-    int32_t hrow[kMoeMaxActive][kMoeMaxTokens];           // by token: row of h, or -1
-    float   share[kMoeMaxActive][kMoeMaxTokens];          // by token: the expert's weight
+    uint32_t ticket; int32_t pad[63];
+    int32_t n; int32_t pad2[63];
     int32_t sel[kMoeMaxTokens][kMoeMaxTopK];              // by token: its experts, largest logit first, -1 = none
     float   sel_w[kMoeMaxTokens][kMoeMaxTopK];
+    MoeActive active[kMoeMaxActive];
 };
 struct MoeLaunch {
     const MoeExpert* experts; const void* router; int router_type; const float* router_bias; int renormalise;
-    int E, top_k, D, F, F_pad;
-    int bh[2], bw[2], gpk[2], zeros[2], nstrips[2];
+    int E, top_k, D, F, F_pad, gather;                      // gather: whether any gate/up layer takes its columns in an order of its own
+    int bh[2], bw[2], gpk[2], zeros[2], nstrips[2], mean_kb[2];
     const int32_t* prow_down;
     const void* x; int64_t ldx; float* y; int64_t ldy; int tokens; int32_t* ids; float* weights;
+    uint32_t* tickets; float* partials;                   // of the strips of the down layers
     MoeRoute* route; float* logits; uint16_t* h;          // h: [2][tokens * top_k][F_pad] fp16, value and remainder
     void* stream;
 };
@@ -126,7 +136,7 @@ struct pivot_qfc_plan {
 
 struct pivot_moe_plan {
     std::vector<const pivot_qfc_plan_t*> gate_up, down;
-    int E = 0, top_k = 0, D = 0, F = 0, router_type = 0, renormalise = 0, device = -1;
+    int E = 0, top_k = 0, D = 0, F = 0, router_type = 0, renormalise = 0, gather = 0, device = -1;
     float eps = 0.f;
     char* dev_base = nullptr;
     pivot::MoeExpert* experts = nullptr; void* router = nullptr; float* router_bias = nullptr; float* norm_weight = nullptr;

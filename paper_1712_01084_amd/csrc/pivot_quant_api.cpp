@@ -62,7 +62,7 @@ int upload(pivot_qfc_plan_t* p, const uint8_t* codes, const void* scales, const 
     const Piece pieces[] = {
         {nullptr, units * kQUnitBytes, &d.codes},
         {nullptr, ns * 2, (void**)&d.scales},
-        {nullptr, h.has_zeros ? ns : 0, (void**)&d.zoff},
+        {nullptr, h.has_zeros ? ns : 0, (void**)&d.zeros},
         {h.kb_ptr.data(), h.kb_ptr.size() * 4, (void**)&d.kb_ptr},
         {h.pieces.data(), h.pieces.size() * 4, (void**)&d.pieces},
         {h.chunks.data(), h.chunks.size() * 4, (void**)&d.chunks},
@@ -82,7 +82,7 @@ int upload(pivot_qfc_plan_t* p, const uint8_t* codes, const void* scales, const 
         if (q.src && (rc = put(mem.p + off, q.src, q.bytes)) != PIVOT_OK) { d = QfcDev{}; return rc; }
         off += align_up(q.bytes + 1, 256);
     }
-    if (!h.has_zeros) d.zoff = nullptr;
+    if (!h.has_zeros) d.zeros = nullptr;
     const size_t code_bytes = (size_t)h.d.M * ((h.d.K + 1) / 2), ngroups = (size_t)h.d.M * ((h.d.K + h.d.group - 1) / h.d.group);
     const size_t o1 = align_up(code_bytes, 256), o2 = o1 + align_up(ngroups * 2, 256), o3 = o2 + (zeros ? align_up(ngroups, 256) : 0);
     if (h.KB > 0) {
@@ -117,11 +117,14 @@ int run_norm(const pivot_norm_args& a, const int32_t* order, void* stream) {
     return launch_norm(L);
 }
 
-struct MoeScratch { size_t route, logits, h, x, total; };
+struct MoeScratch { size_t route, tickets, logits, partials, h, x, total; };   // counters first: their place does not depend on the tokens
 MoeScratch moe_scratch(const pivot_moe_plan_t* p, int tokens) {
     MoeScratch s{};
-    s.logits = align_up(sizeof(MoeRoute), 256);
-    s.h = s.logits + align_up((size_t)tokens * p->E * 4, 256);
+    const size_t strips = p->down[0]->host.M_pad / kQStrip;
+    s.tickets = align_up(sizeof(MoeRoute), 256);
+    s.logits = s.tickets + strips * kQTicketStride * 4;
+    s.partials = s.logits + align_up((size_t)tokens * p->E * 4, 256);
+    s.h = s.partials + align_up(strips * kMoeMaxParts * kQStrip * tokens * 4, 256);
     s.x = s.h + align_up((size_t)2 * tokens * p->top_k * p->down[0]->host.K_pad * 2, 256);
     s.total = s.x + (p->norm_weight ? align_up((size_t)tokens * align_up(p->D, 8) * 2, 256) : 0);
     return s;
@@ -173,7 +176,7 @@ void pivot_qfc_plan_destroy(pivot_qfc_plan_t* plan) {
 
 size_t pivot_qfc_workspace_bytes(const pivot_qfc_plan_t* plan, int batch) {
     if (!plan || batch < 1) return 0;
-    return qfc_ticket_bytes(plan->host) + qfc_partial_bytes(plan->host, batch);
+    return qfc_ticket_bytes(plan->host) + qfc_partial_bytes(plan->host, batch) + qfc_copy_bytes(plan->host, batch);
 }
 
 int pivot_qfc_run(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, int64_t ldx, const float* xscale_dev, float* y_dev, int64_t ldy,
@@ -189,13 +192,13 @@ int pivot_qfc_run(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, in
     const QfcHost& h = plan->host;
     if (ldx < h.d.K || ldy < h.d.M) { set_error("ldx/ldy smaller than K/M"); return PIVOT_E_SHAPE; }
     if (!aligned_to(x_dev, type_size(xtype)) || !aligned_to(y_dev, 4) || !aligned_to(xscale_dev, 4)) { set_error("x, xscale and y must be aligned to their type"); return PIVOT_E_SHAPE; }
-    const size_t nt = qfc_ticket_bytes(h);
-    int rc = need_workspace(ws_dev, ws_bytes, nt + qfc_partial_bytes(h, batch));
+    const size_t nt = qfc_ticket_bytes(h), np = qfc_partial_bytes(h, batch);
+    int rc = need_workspace(ws_dev, ws_bytes, nt + np + qfc_copy_bytes(h, batch));
     if (rc != PIVOT_OK) return rc;
     QfcLaunch L{};
     L.h = &h; L.d = &plan->dev; L.x = x_dev; L.xtype = xtype; L.ldx = ldx; L.xscale = xscale_dev; L.block_order = flags & PIVOT_QFC_X_BLOCK_ORDER;
     L.y = y_dev; L.ldy = ldy; L.batch = batch; L.tickets = static_cast<uint32_t*>(ws_dev);
-    L.partials = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + nt); L.stream = stream;
+    L.partials = reinterpret_cast<float*>(static_cast<char*>(ws_dev) + nt); L.xcopy = static_cast<char*>(ws_dev) + nt + np; L.stream = stream;
     return launch_qfc(L);
 }
 
@@ -295,9 +298,12 @@ int pivot_moe_plan(const pivot_moe_desc* desc, const pivot_qfc_plan_t* const* ga
         for (int i = 0; i < F; ++i) hdst[(size_t)e * npairs + i] = d.invpcol[u.prow_pad[2 * i] / 2];
         const QfcDev* dev[2] = {&gate_up[e]->dev, &down[e]->dev};
         for (int q = 0; q < 2; ++q) {
-            ex[e].codes[q] = dev[q]->codes; ex[e].scales[q] = dev[q]->scales; ex[e].zoff[q] = dev[q]->zoff; ex[e].kb_ptr[q] = dev[q]->kb_ptr;
+            ex[e].codes[q] = dev[q]->codes; ex[e].scales[q] = dev[q]->scales; ex[e].zeros[q] = dev[q]->zeros; ex[e].kb_ptr[q] = dev[q]->kb_ptr;
             ex[e].pieces[q] = dev[q]->pieces; ex[e].bias[q] = dev[q]->bias_p;
+            const QfcHost& l = q ? d : u;
+            ex[e].whole[q] = l.whole ? l.max_kb : 0;
         }
+        p->gather |= !u.identity_cols;
         ex[e].pcol = u.identity_cols ? nullptr : gate_up[e]->dev.pcol_pad;
         ex[e].hdst = hdst_dev + (size_t)e * npairs;
     }
@@ -357,10 +363,13 @@ int pivot_moe_run(const pivot_moe_plan_t* plan, const void* x_dev, int xtype, in
     const QfcHost* hs[2] = {&plan->gate_up[0]->host, &plan->down[0]->host};
     for (int q = 0; q < 2; ++q) {
         L.bh[q] = hs[q]->d.bh; L.bw[q] = hs[q]->d.bw; L.gpk[q] = hs[q]->gpk; L.zeros[q] = hs[q]->has_zeros; L.nstrips[q] = hs[q]->M_pad / kQStrip;
+        L.mean_kb[q] = hs[q]->KB / hs[q]->nbr;
     }
+    L.gather = plan->gather;
     L.experts = plan->experts; L.router = plan->router; L.router_type = plan->router_type; L.router_bias = plan->router_bias; L.renormalise = plan->renormalise;
     L.E = plan->E; L.top_k = plan->top_k; L.D = plan->D; L.F = plan->F; L.F_pad = hs[1]->K_pad; L.prow_down = plan->down[0]->dev.prow_pad;
     L.y = y_dev; L.ldy = ldy; L.tokens = tokens; L.ids = ids_dev; L.weights = weights_dev;
+    L.tickets = reinterpret_cast<uint32_t*>(ws + s.tickets); L.partials = reinterpret_cast<float*>(ws + s.partials);
     L.route = reinterpret_cast<MoeRoute*>(ws + s.route); L.logits = reinterpret_cast<float*>(ws + s.logits); L.h = reinterpret_cast<uint16_t*>(ws + s.h);
     L.stream = stream;
     return launch_moe(L);

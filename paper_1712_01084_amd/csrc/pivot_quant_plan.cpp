@@ -16,16 +16,19 @@ static bool invert(const int32_t* p, int n, std::vector<int32_t>& inv) {
     return true;
 }
 
-// Work items: whole block rows where they fill the device.  A row in pieces pays a hand-over between workgroups of about
-// 1.2 us, so it is cut only where fewer than 256 strips of at least 32 blocks (32 KB) each would leave compute units
-// idle, or where the longest row has at least four times the average (then pieces of twice the average, at least 16).
+// Work items: whole block rows where they fill the device.  A row in pieces pays a hand-over between workgroups of 0.8 us,
+// so it is cut only into pieces of at least 32 blocks (32 KB per strip) and while they leave half of 256 compute units
+// idle: us at batch 1, whole / pieces of 64 / 32 / 16 blocks, dense, 2048x4096 4.7 / - / 4.7 / 5.5, 512x16384 9.2 / 7.5 / 6.5 /
+// 7.2, 2048x16384 10.4 / 9.0 / 9.5 / 11.0, 3000x16384 10.7 / 11.4 / 12.0 / 15.9.  Or where the longest row has 64 blocks and
+// four times the average (then pieces of twice the average, at least 16): 16384x8192, 10 % kept, rows 1 : 30, 10.5 / 10.5 /
+// 8.7 / 7.8.
 static int choose_chunk_blocks(const QfcHost& h) {
     if (h.d.chunk_blocks > 0) return h.d.chunk_blocks;
     const int strips = std::max(1, h.nbr * h.strips()), most = std::max(1, h.max_kb);
     int parts = 1;
-    while (strips * parts < 256 && most / (2 * parts) >= 16) parts *= 2;
+    while (strips * parts * 2 <= 256 && most / (2 * parts) >= 32) parts *= 2;
     int ck = (most + parts - 1) / parts;
-    if ((long long)most * h.nbr >= 4LL * h.KB) ck = std::min(ck, std::max(16, 2 * ((h.KB + h.nbr - 1) / h.nbr)));
+    if (most >= 64 && (long long)most * h.nbr >= 4LL * h.KB) ck = std::min(ck, std::max(16, 2 * ((h.KB + h.nbr - 1) / h.nbr)));
     return ck;
 }
 
@@ -79,6 +82,7 @@ int build_qfc_host(const pivot_qfc_desc& d, const uint8_t* zeros, int64_t groups
     }
     h.T = h.row_ptr[h.nbr];
     h.KB = h.kb_ptr[h.nbr];
+    h.whole = (int64_t)h.T == (int64_t)h.nbr * h.nbc;
 
     h.chunk_blocks = choose_chunk_blocks(h);
     struct Chunk { int row, b, e, first, parts, slot; };

@@ -77,8 +77,8 @@ def test_runs_that_are_refused():
         _refused(B.PIVOT_E_NO_DEVICE, B.pivot_qfc_run, p, 1024, B.PIVOT_F16, 100, None, 1024, 40, 1, None, 0)
         _refused(B.PIVOT_E_NULL, B.pivot_qfc_run, None, 1024, B.PIVOT_F16, 100, None, 1024, 40, 1, None, 0)
         _refused(B.PIVOT_E_NO_DEVICE, B.pivot_norm_run, 1024, B.PIVOT_F32, 100, 1024, B.PIVOT_F32, 100, 1, 100, order=p)
-        assert B.pivot_qfc_kernel_name(p, B.PIVOT_F16, 1).startswith("pivot::qfc_kernel<false")
-        assert B.pivot_qfc_kernel_name(p, B.PIVOT_Q8, 64).startswith("pivot::qfc_kernel<true")
+        assert B.pivot_qfc_kernel_name(p, B.PIVOT_F16, 1).startswith("pivot::qfc_rows_kernel<false")
+        assert B.pivot_qfc_kernel_name(p, B.PIVOT_Q8, 64).startswith("pivot::qfc_frag_kernel<true")
         _refused(B.PIVOT_E_SHAPE, B.pivot_qfc_kernel_name, p, B.PIVOT_F16, 65)
         _refused(B.PIVOT_E_UNSUPPORTED, B.pivot_qfc_kernel_name, p, B.PIVOT_F32, 1)
         assert B.pivot_qfc_workspace_bytes(p, 0) == 0 and B.pivot_qfc_workspace_bytes(None, 1) == 0
