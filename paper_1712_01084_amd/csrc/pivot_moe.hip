@@ -57,22 +57,27 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // 16 wavefronts: TP tokens (the number of tokens, to the next power of two), 16 / TP wavefronts to each for the logit of
-// expert blockIdx.x; in the last workgroup to arrive a wavefront per token for the choice.
-template <typename RT, int TP>
+// expert blockIdx.x; in the last workgroup to arrive a wavefront per token for the choice, NQ experts to
+// a lane.  ONE: a single workgroup, an expert per wavefront in turn, which saves the logits' way through memory.
+template <typename RT, int TP, int NQ, bool ONE>
 __global__ void __launch_bounds__(kRouterThreads) moe_router_kernel(MoeLaunch a, int vec) {
-    constexpr int S = 16 / TP;
-    __shared__ float s_red[16];
+    constexpr int S = 16 / TP, NW = sizeof(MoeExpert) / 8, NE = (64 * NQ * NW + kRouterThreads - 1) / kRouterThreads;
+    __shared__ float s_red[16], s_logit[ONE ? TP : 1][ONE ? 64 * NQ : 1];
     __shared__ int   s_sel[kMoeMaxTokens][kMoeMaxTopK];
     __shared__ float s_w[kMoeMaxTokens][kMoeMaxTopK];
     __shared__ int   s_mask[kMoeMaxExperts], s_at[kMoeMaxExperts], s_base[4], s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = q_wave(), e = blockIdx.x, T = a.tokens, E = a.E, K = a.top_k;
-    {
+    // the experts' layers, which the last workgroup will put beside what it finds, are asked for now
+    unsigned long long layers[NE];
+    #pragma unroll
+    for (int i = 0; i < NE; ++i) layers[i] = tid + i * kRouterThreads < E * NW ? gload<unsigned long long>((const unsigned long long*)a.experts + tid + i * kRouterThreads) : 0;
+    if constexpr (!ONE) {
         const int t = wave % TP;
         const RT* w = reinterpret_cast<const RT*>(a.router) + (long long)e * a.D;
         const _Float16* x = reinterpret_cast<const _Float16*>(a.x) + t * a.ldx;
         float acc = 0.f;
         if (t < T)
-            #pragma unroll 2
+            #pragma unroll 4
             for (int c = ((wave / TP) * 64 + lane) * 8; c < a.D; c += S * 512) {
                 float wv[8], xv[8];
                 router_load8(w, c, a.D, vec, wv);
@@ -82,17 +87,40 @@ __global__ void __launch_bounds__(kRouterThreads) moe_router_kernel(MoeLaunch a,
             }
         acc = wave_sum(acc);
         if (lane == 0) s_red[wave] = acc;
+    } else {
+        for (int e1 = wave; e1 < E; e1 += 16) {
+            const RT* w = reinterpret_cast<const RT*>(a.router) + (long long)e1 * a.D;
+            float acc[TP] = {};
+            #pragma unroll 2
+            for (int c = lane * 8; c < a.D; c += 512) {
+                float wv[8];
+                router_load8(w, c, a.D, vec, wv);
+                #pragma unroll
+                for (int t = 0; t < TP; ++t)
+                    if (t < T) {
+                        float xv[8];
+                        router_load8(reinterpret_cast<const _Float16*>(a.x) + t * a.ldx, c, a.D, vec, xv);
+                        #pragma unroll
+                        for (int i = 0; i < 8; ++i) acc[t] = __builtin_fmaf(wv[i], xv[i], acc[t]);
+                    }
+            }
+            #pragma unroll
+            for (int t = 0; t < TP; ++t) {
+                const float s = wave_sum(acc[t]);
+                if (lane == 0 && t < T) s_logit[t][e1] = s + (a.router_bias ? a.router_bias[e1] : 0.f);
+            }
+        }
     }
     __syncthreads();
-    if (tid < T) {
+    if (!ONE && tid < T) {
         float s = 0.f;
         #pragma unroll
         for (int q = 0; q < S; ++q) s += s_red[q * TP + tid];
         if (a.router_bias) s += a.router_bias[e];
         agent_store(a.logits + tid * E + e, s);
     }
-    if (wave == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the logits are out before the arrival is counted
-    if (tid == 0) {
+    if (!ONE && wave == 0) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // the logits are out before the arrival is counted
+    if (!ONE && tid == 0) {
         const int last = __hip_atomic_fetch_add(&a.route->ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(E - 1);
         if (last) __hip_atomic_store(&a.route->ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s_last = last;
@@ -100,18 +128,18 @@ __global__ void __launch_bounds__(kRouterThreads) moe_router_kernel(MoeLaunch a,
     if (tid < kMoeMaxExperts) s_mask[tid] = 0;
     if (tid < kMoeMaxTokens * kMoeMaxTopK) { (&s_sel[0][0])[tid] = -1; (&s_w[0][0])[tid] = 0.f; }
     __syncthreads();
-    if (!s_last) return;
+    if (!ONE && !s_last) return;
 
     // ---- the last workgroup: who uses what
     if (wave < T) {
         const float ninf = -__builtin_inff();
         const int t = wave;
-        float v[4];
+        float v[NQ];
         int nan = 0;
         #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < NQ; ++q) {
             const int i = lane + 64 * q;
-            v[q] = i < E ? agent_load(a.logits + t * E + i) : ninf;
+            v[q] = i < E ? (ONE ? s_logit[t][i] : agent_load(a.logits + t * E + i)) : ninf;
             nan |= v[q] != v[q];
         }
         if (__any(nan)) {                                // the first top_k experts, with weights that are NaN
@@ -120,21 +148,24 @@ __global__ void __launch_bounds__(kRouterThreads) moe_router_kernel(MoeLaunch a,
             float m = 0.f, s = 0.f, all = 0.f, mine = 0.f;   // mine: lane j's weight of choice j
             int chosen = -1, n = 0;
             for (int j = 0; j < K; ++j) {
-                float top = wave_max(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])));
+                float top = v[0];
+                #pragma unroll
+                for (int q = 1; q < NQ; ++q) top = fmaxf(top, v[q]);
+                top = wave_max(top);
                 if (top == ninf) break;
                 if (j == 0) {
                     m = top;
                     #pragma unroll
-                    for (int q = 0; q < 4; ++q) all += v[q] == ninf ? 0.f : expf(v[q] - m);
+                    for (int q = 0; q < NQ; ++q) all += v[q] == ninf ? 0.f : expf(v[q] - m);
                 }
                 int at = -1;                             // the lowest index among equals
                 #pragma unroll
-                for (int q = 3; q >= 0; --q) {
+                for (int q = NQ - 1; q >= 0; --q) {
                     const unsigned long long b = __ballot(v[q] == top);
                     if (b) at = 64 * q + __builtin_ctzll(b);
                 }
                 #pragma unroll
-                for (int q = 0; q < 4; ++q) if (lane + 64 * q == at) v[q] = ninf;
+                for (int q = 0; q < NQ; ++q) if (lane + 64 * q == at) v[q] = ninf;
                 const float p = expf(top - m);
                 s += p;
                 if (lane == j) { mine = p; chosen = at; }
@@ -181,11 +212,10 @@ __global__ void __launch_bounds__(kRouterThreads) moe_router_kernel(MoeLaunch a,
             act.share[t] = w;
         }
     }
-    // the experts' layers beside them
-    constexpr int NW = sizeof(MoeExpert) / 8;
-    for (int i = tid; i < E * NW; i += kRouterThreads) {
-        const int ex = i / NW;
-        if (s_mask[ex]) reinterpret_cast<unsigned long long*>(&a.route->active[s_at[ex]].ex)[i % NW] = reinterpret_cast<const unsigned long long*>(&a.experts[ex])[i % NW];
+    #pragma unroll
+    for (int i = 0; i < NE; ++i) {
+        const int at = tid + i * kRouterThreads, ex = at / NW;
+        if (at < E * NW && s_mask[ex]) reinterpret_cast<unsigned long long*>(&a.route->active[s_at[ex]].ex)[at % NW] = layers[i];
     }
 }
 
@@ -265,20 +295,22 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
     __shared__ uint8_t s_hrow[kMoeMaxActive][kMoeMaxTokens];
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = q_wave(), T = a.tokens, n_act = a.route->n, parts = gridDim.y, step = W * parts;
+    const int bound = min(a.E, T * a.top_k);            // at most so many experts in use: the loads that follow need not wait for n_act
     const int strip = blockIdx.x, sb = a.bh[1] / kQStrip, br = strip / sb, bw_log2 = 31 - __clz(a.bw[1]);
     if (wave == 0) {                                    // block counts of the experts in use, and their running sum
         int run = 0;
-        for (int base = 0; base < n_act; base += 64) {
+        for (int base = 0; base < bound; base += 64) {
             const int i = base + lane;
             int nkb = 0;
+            const MoeExpert ex = a.route->active[min(i, bound - 1)].ex;
+            const int its = a.route->active[min(i, bound - 1)].mask;
             if (i < n_act) {
-                const MoeExpert& ex = a.route->active[i].ex;
                 const int whole = ex.whole[1], kb0 = whole ? br * whole : ex.kb_ptr[1][br];
                 nkb = whole ? whole : ex.kb_ptr[1][br + 1] - kb0;
                 const size_t unit0 = (size_t)kb0 * sb + (size_t)(strip % sb) * nkb;
                 s_ex[i] = Down{reinterpret_cast<const u32x4*>(ex.codes[1]) + unit0 * 64, ex.scales[1] + unit0 * GPK * kQStrip,
                                ZP ? ex.zeros[1] + unit0 * GPK * kQStrip : nullptr, whole ? nullptr : ex.pieces[1] + ((size_t)kb0 << (7 - bw_log2))};
-                s_mask[i] = a.route->active[i].mask;
+                s_mask[i] = its;
             }
             int s = nkb;
             #pragma unroll
@@ -288,7 +320,7 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
         }
         if (lane == 0) s_cum[0] = 0;
     } else {
-        for (int i = tid - 64; i < n_act * kMoeMaxTokens; i += (W - 1) * 64) {
+        for (int i = tid - 64; i < bound * kMoeMaxTokens; i += (W - 1) * 64) {   // (of unused entries too: what they hold is not used)
             const MoeActive& act = a.route->active[i / kMoeMaxTokens];
             s_share[i / kMoeMaxTokens][i % kMoeMaxTokens] = act.share[i % kMoeMaxTokens];
             s_hrow[i / kMoeMaxTokens][i % kMoeMaxTokens] = (uint8_t)act.hrow[i % kMoeMaxTokens];
@@ -296,6 +328,18 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
     }
     __syncthreads();
     const int units = s_cum[n_act];
+    // what the end needs is asked for now: this thread's (first) output, its experts' biases
+    int e_dst = -1;
+    float e_bias = 0.f;
+    auto bias_of = [&](int i) {
+        float s = 0.f;
+        for (int j = 0; j < a.top_k; ++j) {
+            const int e = a.route->sel[i / 16][j];
+            if (e >= 0) s = __builtin_fmaf(a.route->sel_w[i / 16][j], gload<float>(a.experts[e].bias[1] + strip * 16 + i % 16), s);
+        }
+        return s;
+    };
+    if (tid < 16 * T) { e_dst = a.prow_down[strip * 16 + tid % 16]; e_bias = bias_of(tid); }
     char* xs = smem + wave * (kDownRows<NT> * ROW);
     // this lane's column: a token, its value or (second half of a single tile) its remainder
     const int n = NT == 1 ? (lane & 7) : (lane & 15), second = NT == 1 ? (lane >> 3) & 1 : 0;
@@ -422,16 +466,12 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
         if (!s_last) return;
     }
     for (int i = tid; i < 16 * T; i += W * 64) {
-        const int t = i / 16, r = strip * 16 + i % 16, dst = a.prow_down[r];
-        if (dst < 0) continue;
+        const int dst = i == tid ? e_dst : a.prow_down[strip * 16 + i % 16];
         float s = 0.f;
         if (parts > 1) { for (int q = 0; q < parts; ++q) s += agent_load(mine + q * 16 * T + i); }
         else s = sum_of(i);
-        for (int j = 0; j < a.top_k; ++j) {
-            const int e = a.route->sel[t][j];
-            if (e >= 0) s = __builtin_fmaf(a.route->sel_w[t][j], a.experts[e].bias[1][r], s);
-        }
-        a.y[t * a.ldy + dst] = s;
+        s += i == tid ? e_bias : bias_of(i);
+        if (dst >= 0) a.y[i / 16 * a.ldy + dst] = s;
     }
 }
 
@@ -462,37 +502,45 @@ int up_go(const MoeLaunch& L, int vec) {
     const int most = std::min(2, L.bh[0] / kQStrip), active = std::min(L.E, L.tokens * L.top_k);
     int rs = 1;
     while (rs < most && L.nstrips[0] * active / (2 * rs) >= 512) rs *= 2;
-    if (!(L.gather == 0 && vec && L.D % 8 == 0)) return go(moe_up_kernel<GPK, ZP, 1, false, 4>, 1, 4);
+    if (!(L.gather == 0 && vec && L.D % 8 == 0)) return rs == 1 ? go(moe_up_kernel<GPK, ZP, 1, false, 4>, 1, 4) : go(moe_up_kernel<GPK, ZP, 2, false, 4>, 2, 4);
     return rs == 1 ? go(moe_up_kernel<GPK, ZP, 1, true, 4>, 1, 4) : go(moe_up_kernel<GPK, ZP, 2, true, 4>, 2, 4);
 }
 
 template <int GPK, bool ZP>
 int down_go(const MoeLaunch& L, int) {
     auto go = [&](auto k, int w, int rows) {
-        // Workgroups of a strip: until there are two for every compute unit, with at least two units to a wavefront.
+        // Workgroups of a strip: until there is one for every compute unit, with at least two units to a wavefront.
         const int units = L.mean_kb[1] * std::min(L.E, L.tokens * L.top_k);
         int parts = 1;
-        while (parts < kMoeMaxParts && L.nstrips[1] * parts < 1024 && units >= 4 * w * parts) parts *= 2;
+        while (parts < kMoeMaxParts && L.nstrips[1] * parts < 256 && units >= 4 * w * parts) parts *= 2;
         const size_t smem = (size_t)w * rows * QElem<false>::kRow;      // more than the sums'
         const int rc = reserve(reinterpret_cast<const void*>(k), smem);
         if (rc != PIVOT_OK) return rc;
         hipLaunchKernelGGL(k, dim3(L.nstrips[1], parts), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L);
         return launched();
     };
-    return L.tokens <= 8 ? go(moe_down_kernel<GPK, ZP, 1, 4>, 4, kDownRows<1>) : go(moe_down_kernel<GPK, ZP, 2, 4>, 4, kDownRows<2>);
+    return L.tokens <= 8 ? go(moe_down_kernel<GPK, ZP, 1, 16>, 16, kDownRows<1>) : go(moe_down_kernel<GPK, ZP, 2, 16>, 16, kDownRows<2>);
 }
 
 template <typename RT>
 int router_go(const MoeLaunch& L, int vec) {
-    auto go = [&](auto k) {
-        hipLaunchKernelGGL(k, dim3(L.E), dim3(kRouterThreads), 0, reinterpret_cast<hipStream_t>(L.stream), L, vec);
+    auto go = [&](auto k, int grid) {
+        hipLaunchKernelGGL(k, dim3(grid), dim3(kRouterThreads), 0, reinterpret_cast<hipStream_t>(L.stream), L, vec);
         return launched();
     };
-    if (L.tokens == 1) return go(moe_router_kernel<RT, 1>);
-    if (L.tokens == 2) return go(moe_router_kernel<RT, 2>);
-    if (L.tokens <= 4) return go(moe_router_kernel<RT, 4>);
-    if (L.tokens <= 8) return go(moe_router_kernel<RT, 8>);
-    return go(moe_router_kernel<RT, 16>);
+    auto many = [&](auto nq) {
+        constexpr int NQ = decltype(nq)::value;
+        if (L.tokens == 1) return go(moe_router_kernel<RT, 1, NQ, false>, L.E);
+        if (L.tokens == 2) return go(moe_router_kernel<RT, 2, NQ, false>, L.E);
+        if (L.tokens <= 4) return go(moe_router_kernel<RT, 4, NQ, false>, L.E);
+        if (L.tokens <= 8) return go(moe_router_kernel<RT, 8, NQ, false>, L.E);
+        return go(moe_router_kernel<RT, 16, NQ, false>, L.E);
+    };
+    // One workgroup where a lane has at most 8 pieces of 16 bytes to load (16 experts, 512 columns, 1 token 16.5 -> 15.4 us for
+    // the layer, 8 experts, 1024 columns 15.5 -> 14.7; with 16 pieces even, with 32 up to 9 us behind).
+    const int loads = ((L.E + 15) / 16) * ((L.D + 511) / 512) * (1 + L.tokens);
+    if (L.E <= 64 && L.tokens <= 4 && loads <= 8) return L.tokens == 1 ? go(moe_router_kernel<RT, 1, 1, true>, 1) : go(moe_router_kernel<RT, 4, 1, true>, 1);
+    return L.E <= 64 ? many(std::integral_constant<int, 1>()) : many(std::integral_constant<int, 4>());
 }
 
 #define PIVOT_MOE_PICK(go, which)                                                                                          \

@@ -2,102 +2,147 @@
 //
 //     h = x + res,   out = weight * h / sqrt(mean(h^2) + eps);   8 bits: max |out| / 127 is one step
 //
-// TPR threads share a row and keep it in registers between the two passes (sum of squares and largest weight * h, then
-// the outputs); rows too long for that are read a second time.  The 8-bit codes depend on weight * h / max alone, which is
-// computed in 64 bits: in 32 bits about one code in 10^5 would fall to the other side of the middle between two.
+// TPR threads share a row, eight neighbouring columns each at a time, and keep weight * h in registers between the two
+// passes (sum of squares and largest weight * h, then the outputs); what of a row does not fit there is read a second
+// time.  The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
+// 10^5 would fall to the other side of the middle between two.
+#include <type_traits>
+
 #include "pivot_quant_core.h"
 
 namespace pivot {
 
 namespace {
 
-// Eight (V = 8: neighbouring, aligned) or single elements as floats.
-template <int V>
-__device__ __forceinline__ void norm_load(const void* p, int type, long long at, float (&v)[V]) {
-    if (type == PIVOT_F32) {
-        const float* q = reinterpret_cast<const float*>(p) + at;
-        if (V == 8) {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(q), b = *reinterpret_cast<const f32x4*>(q + 4);
+// Vectors of eight that need no more alignment than their elements have.
+typedef float    f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+typedef _Float16 f16x8_any __attribute__((ext_vector_type(8), aligned(2)));
+
+// Eight neighbouring elements as floats, the first `n` of them real (the others 0).
+__device__ __forceinline__ void norm_load(const void* p, int type, long long at, int n, float (&v)[8]) {
+    if (n >= 8) {
+        if (type == PIVOT_F32) {
+            const f32x4_any a = gload<f32x4_any>((const float*)p + at), b = gload<f32x4_any>((const float*)p + at + 4);
             #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
-        } else v[0] = q[0];
-    } else {
-        const _Float16* q = reinterpret_cast<const _Float16*>(p) + at;
-        if (V == 8) {
-            const f16x8 a = *reinterpret_cast<const f16x8*>(q);
+            for (int i = 0; i < 8; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
+        } else {
+            const f16x8_any a = gload<f16x8_any>((const _Float16*)p + at);
             #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = (float)a[i];
-        } else v[0] = (float)q[0];
+            for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
+        }
+        return;
     }
+    #pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i >= n ? 0.f : (type == PIVOT_F32 ? gload<float>((const float*)p + at + i) : (float)gload<_Float16>((const _Float16*)p + at + i));
 }
 
-template <int V>
-__device__ __forceinline__ void norm_store(void* p, int type, long long at, const float (&v)[V]) {
+__device__ __forceinline__ void norm_store(void* p, int type, long long at, int n, const float (&v)[8]) {
     if (type == PIVOT_F32) {
         float* q = reinterpret_cast<float*>(p) + at;
-        if (V == 8) {
-            *reinterpret_cast<f32x4*>(q) = f32x4{v[0], v[1 % V], v[2 % V], v[3 % V]};
-            *reinterpret_cast<f32x4*>(q + 4) = f32x4{v[4 % V], v[5 % V], v[6 % V], v[7 % V]};
-        } else q[0] = v[0];
+        if (n >= 8) {
+            *reinterpret_cast<f32x4_any*>(q) = f32x4_any{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4_any*>(q + 4) = f32x4_any{v[4], v[5], v[6], v[7]};
+        } else
+            for (int i = 0; i < n; ++i) q[i] = v[i];
     } else {
         _Float16* q = reinterpret_cast<_Float16*>(p) + at;
-        if (V == 8) {
-            f16x8 o;
+        if (n >= 8) {
+            f16x8_any o;
             #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = (_Float16)v[i];
-            *reinterpret_cast<f16x8*>(q) = o;
-        } else q[0] = (_Float16)v[0];
+            for (int i = 0; i < 8; ++i) o[i] = (_Float16)v[i];
+            *reinterpret_cast<f16x8_any*>(q) = o;
+        } else
+            for (int i = 0; i < n; ++i) q[i] = (_Float16)v[i];
     }
 }
 
 // The larger of two, a NaN being larger than anything.
-__device__ __forceinline__ double most_of(double m, double o) { return (o > m || o != o) ? o : m; }
+template <typename T> __device__ __forceinline__ T most_of(T m, T o) { return (o > m || o != o) ? o : m; }
+
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double v) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const unsigned lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, 0xF, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, (long long)(((unsigned long long)hi << 32) | lo));
+}
+__device__ __forceinline__ double lane64(double v, int l) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const unsigned lo = __builtin_amdgcn_readlane((int)b, l), hi = __builtin_amdgcn_readlane((int)(b >> 32), l);
+    return __builtin_bit_cast(double, (long long)(((unsigned long long)hi << 32) | lo));
+}
+// Over the 64 lanes, in every one of them: rows of sixteen by lane permutes, then the four rows.
+template <typename Op>
+__device__ __forceinline__ double wave64(double v, Op op) {
+    v = op(v, dpp64<0xB1>(v));
+    v = op(v, dpp64<0x4E>(v));
+    v = op(v, dpp64<0x141>(v));
+    v = op(v, dpp64<0x140>(v));
+    return op(op(lane64(v, 0), lane64(v, 16)), op(lane64(v, 32), lane64(v, 48)));
+}
 
 }  // namespace
 
-template <bool Q8, int V, int TPR>
+template <bool Q8, int TPR, int KEEP>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch a) {
-    constexpr int NT = TPR < 256 ? 256 : TPR, NW = TPR / 64, KEEP = V == 8 ? 2 : 4;
+    typedef typename std::conditional<Q8, double, float>::type H;   // h and weight * h
+    constexpr int NT = TPR < 256 ? 256 : TPR, NW = TPR / 64;
     __shared__ double s_sum[NT / 64], s_most[NT / 64];
-    const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = q_wave();
     const long long row = (long long)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     if (TPR < 256 && row >= a.rows) return;             // (whole wavefronts: no barrier below for TPR = 64)
     const long long xo = row * a.ldx, ro = row * a.ldr, so = row * a.ldro, oo = row * a.ldo;
-    float kx[KEEP][V], kr[KEEP][V], kw[KEEP][V];
-    double sum = 0.0, most = 0.0;
-    auto fetch = [&](int c, float (&x)[V], float (&r)[V], float (&w)[V]) {
-        norm_load<V>(a.x, a.xtype, xo + c, x);
-        if (a.res) norm_load<V>(a.res, a.rtype, ro + c, r);
-        else for (int i = 0; i < V; ++i) r[i] = 0.f;
-        if (a.weight) norm_load<V>(a.weight, PIVOT_F32, c, w);
-        else for (int i = 0; i < V; ++i) w[i] = 1.f;
+    struct Piece { float x[8], r[8], w[8]; };
+    auto fetch = [&](int c, Piece& p) {
+        const int n = a.cols - c;
+        norm_load(a.x, a.xtype, xo + c, n, p.x);
+        if (a.res) norm_load(a.res, a.rtype, ro + c, n, p.r);
+        if (a.weight) norm_load(a.weight, PIVOT_F32, c, n, p.w);
     };
-    auto measure = [&](const float (&x)[V], const float (&r)[V], const float (&w)[V]) {
+    // 8-bit rows in a layer's block order are put together in LDS: single bytes all over a row would be a line each to the
+    // memory system
+    extern __shared__ __align__(16) char s_row[];
+    const bool assemble = Q8 && a.order && a.lds_rows;
+    int8_t* mine = reinterpret_cast<int8_t*>(s_row) + (threadIdx.x / TPR) * ((a.cols + 15) & ~15);
+    int place[KEEP][8];
+    if (assemble)
         #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const double h = (double)x[i] + (double)r[i];
-            sum += h * h;
-            if (Q8) most = most_of(most, fabs(h * (double)w[i]));
+        for (int k = 0; k < KEEP; ++k)
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) { const int c = (tid + k * TPR) * 8 + i; place[k][i] = c < a.cols ? gload<int>(a.order + c) : 0; }
+    double sum = 0.0, most = 0.0;
+    // h of a piece, and weight * h; the sums on the first pass, what goes back to the residual on the last one
+    auto combine = [&](int c, const Piece& p, H (&hw)[8], bool first, bool last) {
+        float back[8];
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const H h = a.res ? (H)p.x[i] + (H)p.r[i] : (H)p.x[i];
+            back[i] = Q8 ? p.x[i] + p.r[i] : (float)h;
+            hw[i] = a.weight ? h * (H)p.w[i] : h;
+            if (first) {
+                sum = __builtin_fma((double)h, (double)h, sum);
+                if (Q8) most = most_of(most, fabs((double)hw[i]));
+            }
         }
+        if (last && a.res_out) norm_store(a.res_out, a.rtype, so + c, a.cols - c, back);
     };
-    #pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
-        const int c = (tid + k * TPR) * V;
-        if (c < a.cols) { fetch(c, kx[k], kr[k], kw[k]); }
+    H keep[KEEP][8];
+    {
+        Piece p[KEEP];
+        #pragma unroll
+        for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) fetch((tid + k * TPR) * 8, p[k]);
+        #pragma unroll
+        for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) combine((tid + k * TPR) * 8, p[k], keep[k], true, true);
     }
-    #pragma unroll
-    for (int k = 0; k < KEEP; ++k)
-        if ((tid + k * TPR) * V < a.cols) measure(kx[k], kr[k], kw[k]);
-    for (int c = (tid + KEEP * TPR) * V; c < a.cols; c += TPR * V) {
-        float x[V], r[V], w[V];
-        fetch(c, x, r, w);
-        measure(x, r, w);
+    for (int c = (tid + KEEP * TPR) * 8; c < a.cols; c += TPR * 8) {
+        Piece p;
+        H hw[8];
+        fetch(c, p);
+        combine(c, p, hw, true, false);
     }
-    #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        sum += __shfl_xor(sum, m, 64);
-        if (Q8) most = most_of(most, __shfl_xor(most, m, 64));
-    }
+    auto plus = [](double u, double v) { return u + v; };
+    auto larger = [](double u, double v) { return most_of(u, v); };
+    sum = wave64(sum, plus);
+    if (Q8) most = wave64(most, larger);
     if (NW > 1) {
         if (lane == 0) { s_sum[wave] = sum; s_most[wave] = most; }
         __syncthreads();
@@ -110,73 +155,79 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
     const double inv = fine ? 127.0 / most : 0.0;
     if (Q8 && tid == 0) a.scale[row] = fine ? (float)(most * rstd / 127.0) : (most == 0.0 ? 0.f : __builtin_nanf(""));
     const float rs = (float)rstd;
-    auto finish = [&](int c, const float (&x)[V], const float (&r)[V], const float (&w)[V]) {
-        if (a.res_out) {
-            float h[V];
-            #pragma unroll
-            for (int i = 0; i < V; ++i) h[i] = x[i] + r[i];
-            norm_store<V>(a.res_out, a.rtype, so + c, h);
-        }
+    auto finish = [&](int c, const H (&hw)[8], const int* at) {
+        const int n = a.cols - c;
         if (Q8) {
-            union { int8_t b[8]; uint2 u; } o;
+            union { int8_t b[8]; u32x2 u; } o;
             #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const double hw = ((double)x[i] + (double)r[i]) * (double)w[i];
-                o.b[i] = fine ? (int8_t)__double2int_rn(hw * inv) : (int8_t)0;
-            }
+            for (int i = 0; i < 8; ++i) o.b[i] = fine ? (int8_t)__double2int_rn((double)hw[i] * inv) : (int8_t)0;
             int8_t* q = reinterpret_cast<int8_t*>(a.out) + oo;
-            if (a.order) { for (int i = 0; i < V; ++i) q[a.order[c + i]] = o.b[i]; }
-            else if (V == 8) *reinterpret_cast<uint2*>(q + c) = o.u;
-            else q[c] = o.b[0];
+            if (assemble) {
+                #pragma unroll
+                for (int i = 0; i < 8; ++i) if (i < n) mine[at ? at[i] : a.order[c + i]] = o.b[i];
+            } else if (!a.order && n >= 8) {
+                typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+                *reinterpret_cast<u32x2_any*>(q + c) = u32x2_any{o.u[0], o.u[1]};
+            } else
+                #pragma unroll
+                for (int i = 0; i < 8; ++i) if (i < n) q[a.order ? a.order[c + i] : c + i] = o.b[i];
         } else {
-            float v[V];
+            float v[8];
             #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = (x[i] + r[i]) * w[i] * rs;
-            if (a.order) {
-                for (int i = 0; i < V; ++i) {
-                    const float one[1] = {v[i]};
-                    norm_store<1>(a.out, a.otype, oo + a.order[c + i], one);
-                }
-            } else norm_store<V>(a.out, a.otype, oo + c, v);
+            for (int i = 0; i < 8; ++i) v[i] = (float)hw[i] * rs;
+            if (!a.order) norm_store(a.out, a.otype, oo + c, n, v);
+            else
+                #pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < n) {
+                        const long long at = oo + a.order[c + i];
+                        if (a.otype == PIVOT_F32) reinterpret_cast<float*>(a.out)[at] = v[i];
+                        else reinterpret_cast<_Float16*>(a.out)[at] = (_Float16)v[i];
+                    }
         }
     };
     #pragma unroll
-    for (int k = 0; k < KEEP; ++k) {
-        const int c = (tid + k * TPR) * V;
-        if (c < a.cols) finish(c, kx[k], kr[k], kw[k]);
+    for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) finish((tid + k * TPR) * 8, keep[k], place[k]);
+    for (int c = (tid + KEEP * TPR) * 8; c < a.cols; c += TPR * 8) {
+        Piece p;
+        H hw[8];
+        fetch(c, p);
+        combine(c, p, hw, false, true);
+        finish(c, hw, nullptr);
     }
-    for (int c = (tid + KEEP * TPR) * V; c < a.cols; c += TPR * V) {
-        float x[V], r[V], w[V];
-        fetch(c, x, r, w);
-        finish(c, x, r, w);
+    if (assemble) {
+        if (NW > 1) __syncthreads(); else wave_lds_sync();
+        int8_t* q = reinterpret_cast<int8_t*>(a.out) + oo;
+        typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+        for (int c = tid * 16; c < a.cols; c += TPR * 16) {
+            if (c + 16 <= a.cols) { const u32x4 v = *reinterpret_cast<const u32x4*>(mine + c); *reinterpret_cast<u32x4_any*>(q + c) = u32x4_any{v[0], v[1], v[2], v[3]}; }
+            else for (int i = c; i < a.cols; ++i) q[i] = mine[i];
+        }
     }
 }
 
 namespace {
 
-template <bool Q8, int V>
-int norm_go(const NormLaunch& a) {
+template <bool Q8>
+int norm_go(NormLaunch a) {
     hipStream_t st = reinterpret_cast<hipStream_t>(a.stream);
-    if (a.cols <= 64 * V)       hipLaunchKernelGGL((norm_kernel<Q8, V, 64>), dim3((a.rows + 3) / 4), dim3(256), 0, st, a);
-    else if (a.cols <= 512 * V) hipLaunchKernelGGL((norm_kernel<Q8, V, 256>), dim3(a.rows), dim3(256), 0, st, a);
-    else                        hipLaunchKernelGGL((norm_kernel<Q8, V, 1024>), dim3(a.rows), dim3(1024), 0, st, a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
-    return PIVOT_OK;
-}
-
-bool whole(const void* p, int type, int64_t ld, int rows) {     // whether rows are whole pieces of eight
-    const int piece = type == PIVOT_Q8 ? 8 : 16, es = type == PIVOT_Q8 ? 1 : elem_size(type);
-    return !p || (reinterpret_cast<uintptr_t>(p) % piece == 0 && (rows == 1 || ld * es % piece == 0));
+    auto go = [&](auto k, int per, int threads) {
+        const size_t row = align_up(a.cols, 16) * per;
+        a.lds_rows = Q8 && a.order && row <= 60 * 1024;
+        hipLaunchKernelGGL(k, dim3((unsigned)(((long long)a.rows + per - 1) / per)), dim3(threads), a.lds_rows ? row : 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
+        return PIVOT_OK;
+    };
+    const bool many = a.rows >= 512;
+    if (a.cols <= 64 * 8 && (many || a.cols <= 64)) return go(norm_kernel<Q8, 64, 1>, 4, 256);
+    if (a.cols <= 256 * 8) return go(norm_kernel<Q8, 256, 1>, 1, 256);
+    if (a.cols <= 512 * 8 && many) return go(norm_kernel<Q8, 256, 2>, 1, 256);
+    return a.cols <= 1024 * 8 ? go(norm_kernel<Q8, 1024, 1>, 1, 1024) : go(norm_kernel<Q8, 1024, 2>, 1, 1024);
 }
 
 }  // namespace
 
-int launch_norm(const NormLaunch& a) {
-    const bool v8 = a.cols % 8 == 0 && whole(a.x, a.xtype, a.ldx, a.rows) && whole(a.res, a.rtype, a.ldr, a.rows) && whole(a.res_out, a.rtype, a.ldro, a.rows) &&
-                    whole(a.weight, PIVOT_F32, 0, 1) && (a.order || whole(a.out, a.otype, a.ldo, a.rows));
-    if (a.otype == PIVOT_Q8) return v8 ? norm_go<true, 8>(a) : norm_go<true, 1>(a);
-    return v8 ? norm_go<false, 8>(a) : norm_go<false, 1>(a);
-}
+int launch_norm(const NormLaunch& a) { return a.otype == PIVOT_Q8 ? norm_go<true>(a) : norm_go<false>(a); }
 
 }  // namespace pivot
