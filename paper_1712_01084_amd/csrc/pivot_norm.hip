@@ -43,7 +43,8 @@ __device__ __forceinline__ void norm_store(void* p, int type, long long at, int 
             *reinterpret_cast<f32x4_any*>(q) = f32x4_any{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4_any*>(q + 4) = f32x4_any{v[4], v[5], v[6], v[7]};
         } else
-            for (int i = 0; i < n; ++i) q[i] = v[i];
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < n) q[i] = v[i];
     } else {
         _Float16* q = reinterpret_cast<_Float16*>(p) + at;
         if (n >= 8) {
@@ -52,7 +53,8 @@ __device__ __forceinline__ void norm_store(void* p, int type, long long at, int 
             for (int i = 0; i < 8; ++i) o[i] = (_Float16)v[i];
             *reinterpret_cast<f16x8_any*>(q) = o;
         } else
-            for (int i = 0; i < n; ++i) q[i] = (_Float16)v[i];
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) if (i < n) q[i] = (_Float16)v[i];
     }
 }
 
@@ -80,17 +82,39 @@ __device__ __forceinline__ double wave64(double v, Op op) {
     return op(op(lane64(v, 0), lane64(v, 16)), op(lane64(v, 32), lane64(v, 48)));
 }
 
+// v * inv to the nearest integer, ties to even: the low word of the product + 1.5 * 2^52.  The product is rounded before the
+// addition, so that what lies in the middle between two codes stays there.
+__device__ __forceinline__ int code_of(double v, double inv) {
+    #pragma clang fp contract(off)
+    const double p = v * inv;
+    return (int)__builtin_bit_cast(long long, p + 6755399441055744.0);
+}
+
 }  // namespace
 
-template <bool Q8, int TPR, int KEEP>
+// Q8: weight * h in 64 bits, else in 32.  Of the 64-bit operations (a large part of the time of 8-bit rows from fp16) a column
+// costs nine: three conversions, h, h^2 into the sum, weight * h, the maximum, and two for the code.
+template <bool Q8, bool ORDER, int TPR, int KEEP>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch a) {
-    typedef typename std::conditional<Q8, double, float>::type H;   // h and weight * h
     constexpr int NT = TPR < 256 ? 256 : TPR, NW = TPR / 64;
+    typedef typename std::conditional<Q8, double, float>::type H;   // h and weight * h
     __shared__ double s_sum[NT / 64], s_most[NT / 64];
+    extern __shared__ __align__(16) char s_row[];       // the output row, where it is put together there
     const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = q_wave();
     const long long row = (long long)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     if (TPR < 256 && row >= a.rows) return;             // (whole wavefronts: no barrier below for TPR = 64)
     const long long xo = row * a.ldx, ro = row * a.ldr, so = row * a.ldro, oo = row * a.ldo;
+    const int es = Q8 ? 1 : (a.otype == PIVOT_F32 ? 4 : 2);
+    // rows in a layer's block order are put together in LDS: single elements all over a row would be a line each to the
+    // memory system
+    char* mine = s_row + (threadIdx.x / TPR) * ((a.cols * es + 15) & ~15);
+    int place[ORDER ? KEEP : 1][8];
+    if (ORDER)
+        #pragma unroll
+        for (int k = 0; k < KEEP; ++k)
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) { const int c = (tid + k * TPR) * 8 + i; place[k][i] = c < a.cols ? gload<int>(a.order + c) : 0; }
+
     struct Piece { float x[8], r[8], w[8]; };
     auto fetch = [&](int c, Piece& p) {
         const int n = a.cols - c;
@@ -98,29 +122,23 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         if (a.res) norm_load(a.res, a.rtype, ro + c, n, p.r);
         if (a.weight) norm_load(a.weight, PIVOT_F32, c, n, p.w);
     };
-    // 8-bit rows in a layer's block order are put together in LDS: single bytes all over a row would be a line each to the
-    // memory system
-    extern __shared__ __align__(16) char s_row[];
-    const bool assemble = Q8 && a.order && a.lds_rows;
-    int8_t* mine = reinterpret_cast<int8_t*>(s_row) + (threadIdx.x / TPR) * ((a.cols + 15) & ~15);
-    int place[KEEP][8];
-    if (assemble)
-        #pragma unroll
-        for (int k = 0; k < KEEP; ++k)
-            #pragma unroll
-            for (int i = 0; i < 8; ++i) { const int c = (tid + k * TPR) * 8 + i; place[k][i] = c < a.cols ? gload<int>(a.order + c) : 0; }
     double sum = 0.0, most = 0.0;
-    // h of a piece, and weight * h; the sums on the first pass, what goes back to the residual on the last one
+    float bad = 0.f;                                    // NaN once anything is infinite or NaN
+    // weight * h of a piece; the sums on the first pass, what goes back to the residual on the last one
     auto combine = [&](int c, const Piece& p, H (&hw)[8], bool first, bool last) {
         float back[8];
         #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const H h = a.res ? (H)p.x[i] + (H)p.r[i] : (H)p.x[i];
-            back[i] = Q8 ? p.x[i] + p.r[i] : (float)h;
-            hw[i] = a.weight ? h * (H)p.w[i] : h;
+            const float x = p.x[i], r = a.res ? p.r[i] : 0.f, w = a.weight ? p.w[i] : 1.f;
+            const H h = a.res ? (H)x + (H)r : (H)x;
+            back[i] = x + r;
+            hw[i] = a.weight ? h * (H)w : h;
             if (first) {
                 sum = __builtin_fma((double)h, (double)h, sum);
-                if (Q8) most = most_of(most, fabs((double)hw[i]));
+                if (Q8) {
+                    most = __builtin_fmax(most, __builtin_fabs((double)hw[i]));
+                    bad = __builtin_fmaf(x, 0.f, __builtin_fmaf(r, 0.f, __builtin_fmaf(w, 0.f, bad)));
+                }
             }
         }
         if (last && a.res_out) norm_store(a.res_out, a.rtype, so + c, a.cols - c, back);
@@ -139,6 +157,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         fetch(c, p);
         combine(c, p, hw, true, false);
     }
+    if (Q8 && bad != bad) most = __builtin_nan("");
     auto plus = [](double u, double v) { return u + v; };
     auto larger = [](double u, double v) { return most_of(u, v); };
     sum = wave64(sum, plus);
@@ -153,41 +172,47 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
     const double rstd = 1.0 / sqrt(sum / a.cols + (double)a.eps);
     const bool fine = most > 0.0 && most < __builtin_inf();
     const double inv = fine ? 127.0 / most : 0.0;
-    if (Q8 && tid == 0) a.scale[row] = fine ? (float)(most * rstd / 127.0) : (most == 0.0 ? 0.f : __builtin_nanf(""));
     const float rs = (float)rstd;
+    if (Q8 && tid == 0) a.scale[row] = fine ? (float)(most * rstd / 127.0) : (most == 0.0 ? 0.f : __builtin_nanf(""));
     auto finish = [&](int c, const H (&hw)[8], const int* at) {
         const int n = a.cols - c;
-        if (Q8) {
-            union { int8_t b[8]; u32x2 u; } o;
+        if constexpr (Q8) {
+            int code[8];
             #pragma unroll
-            for (int i = 0; i < 8; ++i) o.b[i] = fine ? (int8_t)__double2int_rn((double)hw[i] * inv) : (int8_t)0;
+            for (int i = 0; i < 8; ++i) {
+                code[i] = fine ? code_of(hw[i], inv) : 0;
+            }
             int8_t* q = reinterpret_cast<int8_t*>(a.out) + oo;
-            if (assemble) {
+            if (ORDER) {
+                int8_t* to = a.lds_rows ? reinterpret_cast<int8_t*>(mine) : q;
                 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (i < n) mine[at ? at[i] : a.order[c + i]] = o.b[i];
-            } else if (!a.order && n >= 8) {
+                for (int i = 0; i < 8; ++i) if (i < n) to[at ? at[i] : a.order[c + i]] = (int8_t)code[i];
+            } else if (n >= 8) {
                 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
-                *reinterpret_cast<u32x2_any*>(q + c) = u32x2_any{o.u[0], o.u[1]};
+                auto four = [&](int i) { return (code[i] & 255u) | (code[i + 1] & 255u) << 8 | (code[i + 2] & 255u) << 16 | (uint32_t)code[i + 3] << 24; };
+                *reinterpret_cast<u32x2_any*>(q + c) = u32x2_any{four(0), four(4)};
             } else
                 #pragma unroll
-                for (int i = 0; i < 8; ++i) if (i < n) q[a.order ? a.order[c + i] : c + i] = o.b[i];
+                for (int i = 0; i < 8; ++i) if (i < n) q[c + i] = (int8_t)code[i];
         } else {
             float v[8];
             #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (float)hw[i] * rs;
-            if (!a.order) norm_store(a.out, a.otype, oo + c, n, v);
-            else
+            for (int i = 0; i < 8; ++i) v[i] = hw[i] * rs;
+            if (!ORDER) norm_store(a.out, a.otype, oo + c, n, v);
+            else {
+                char* to = a.lds_rows ? mine : reinterpret_cast<char*>(a.out) + oo * es;
                 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     if (i < n) {
-                        const long long at = oo + a.order[c + i];
-                        if (a.otype == PIVOT_F32) reinterpret_cast<float*>(a.out)[at] = v[i];
-                        else reinterpret_cast<_Float16*>(a.out)[at] = (_Float16)v[i];
+                        const int d = at ? at[i] : a.order[c + i];
+                        if (a.otype == PIVOT_F32) reinterpret_cast<float*>(to)[d] = v[i];
+                        else reinterpret_cast<_Float16*>(to)[d] = (_Float16)v[i];
                     }
+            }
         }
     };
     #pragma unroll
-    for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) finish((tid + k * TPR) * 8, keep[k], place[k]);
+    for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) finish((tid + k * TPR) * 8, keep[k], ORDER ? place[k] : nullptr);
     for (int c = (tid + KEEP * TPR) * 8; c < a.cols; c += TPR * 8) {
         Piece p;
         H hw[8];
@@ -195,39 +220,43 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         combine(c, p, hw, false, true);
         finish(c, hw, nullptr);
     }
-    if (assemble) {
+    if (ORDER && a.lds_rows) {
         if (NW > 1) __syncthreads(); else wave_lds_sync();
-        int8_t* q = reinterpret_cast<int8_t*>(a.out) + oo;
+        char* q = reinterpret_cast<char*>(a.out) + oo * es;
+        const int bytes = a.cols * es;
         typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
-        for (int c = tid * 16; c < a.cols; c += TPR * 16) {
-            if (c + 16 <= a.cols) { const u32x4 v = *reinterpret_cast<const u32x4*>(mine + c); *reinterpret_cast<u32x4_any*>(q + c) = u32x4_any{v[0], v[1], v[2], v[3]}; }
-            else for (int i = c; i < a.cols; ++i) q[i] = mine[i];
+        for (int b = tid * 16; b < bytes; b += TPR * 16) {
+            if (b + 16 <= bytes) { const u32x4 v = *reinterpret_cast<const u32x4*>(mine + b); *reinterpret_cast<u32x4_any*>(q + b) = u32x4_any{v[0], v[1], v[2], v[3]}; }
+            else for (int i = b; i < bytes; ++i) q[i] = mine[i];
         }
     }
 }
 
 namespace {
 
-template <bool Q8>
+template <bool Q8, bool ORDER>
 int norm_go(NormLaunch a) {
     hipStream_t st = reinterpret_cast<hipStream_t>(a.stream);
     auto go = [&](auto k, int per, int threads) {
-        const size_t row = align_up(a.cols, 16) * per;
-        a.lds_rows = Q8 && a.order && row <= 60 * 1024;
+        const size_t row = align_up((size_t)a.cols * (a.otype == PIVOT_Q8 ? 1 : elem_size(a.otype)), 16) * per;
+        a.lds_rows = ORDER && row <= 60 * 1024;          // (longer rows: element by element)
         hipLaunchKernelGGL(k, dim3((unsigned)(((long long)a.rows + per - 1) / per)), dim3(threads), a.lds_rows ? row : 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
         return PIVOT_OK;
     };
-    const bool many = a.rows >= 512;
-    if (a.cols <= 64 * 8 && (many || a.cols <= 64)) return go(norm_kernel<Q8, 64, 1>, 4, 256);
-    if (a.cols <= 256 * 8) return go(norm_kernel<Q8, 256, 1>, 1, 256);
-    if (a.cols <= 512 * 8 && many) return go(norm_kernel<Q8, 256, 2>, 1, 256);
-    return a.cols <= 1024 * 8 ? go(norm_kernel<Q8, 1024, 1>, 1, 1024) : go(norm_kernel<Q8, 1024, 2>, 1, 1024);
+    const bool many = a.rows >= 512;                      // rows enough to fill the device with few threads each
+    if (a.cols <= 64 * 8 && (many || a.cols <= 64)) return go(norm_kernel<Q8, ORDER, 64, 1>, 4, 256);
+    if (a.cols <= 256 * 8) return go(norm_kernel<Q8, ORDER, 256, 1>, 1, 256);
+    if (a.cols <= 512 * 8 && many) return go(norm_kernel<Q8, ORDER, 512, 1>, 1, 512);
+    return a.cols <= 1024 * 8 ? go(norm_kernel<Q8, ORDER, 1024, 1>, 1, 1024) : go(norm_kernel<Q8, ORDER, 1024, 2>, 1, 1024);
 }
 
 }  // namespace
 
-int launch_norm(const NormLaunch& a) { return a.otype == PIVOT_Q8 ? norm_go<true>(a) : norm_go<false>(a); }
+int launch_norm(const NormLaunch& a) {
+    if (a.otype == PIVOT_Q8) return a.order ? norm_go<true, true>(a) : norm_go<true, false>(a);
+    return a.order ? norm_go<false, true>(a) : norm_go<false, false>(a);
+}
 
 }  // namespace pivot
