@@ -58,9 +58,6 @@ __device__ __forceinline__ void norm_store(void* p, int type, long long at, int 
     }
 }
 
-// The larger of two, a NaN being larger than anything.
-template <typename T> __device__ __forceinline__ T most_of(T m, T o) { return (o > m || o != o) ? o : m; }
-
 template <int CTRL>
 __device__ __forceinline__ double dpp64(double v) {
     const long long b = __builtin_bit_cast(long long, v);
@@ -120,7 +117,13 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         const int n = a.cols - c;
         norm_load(a.x, a.xtype, xo + c, n, p.x);
         if (a.res) norm_load(a.res, a.rtype, ro + c, n, p.r);
+        else
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) p.r[i] = 0.f;
         if (a.weight) norm_load(a.weight, PIVOT_F32, c, n, p.w);
+        else
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) p.w[i] = 1.f;
     };
     double sum = 0.0, most = 0.0;
     float bad = 0.f;                                    // NaN once anything is infinite or NaN
@@ -129,10 +132,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         float back[8];
         #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float x = p.x[i], r = a.res ? p.r[i] : 0.f, w = a.weight ? p.w[i] : 1.f;
-            const H h = a.res ? (H)x + (H)r : (H)x;
+            const float x = p.x[i], r = p.r[i], w = p.w[i];
+            const H h = (H)x + (H)r;
             back[i] = x + r;
-            hw[i] = a.weight ? h * (H)w : h;
+            hw[i] = h * (H)w;
             if (first) {
                 sum = __builtin_fma((double)h, (double)h, sum);
                 if (Q8) {
@@ -157,23 +160,28 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         fetch(c, p);
         combine(c, p, hw, true, false);
     }
-    if (Q8 && bad != bad) most = __builtin_nan("");
-    auto plus = [](double u, double v) { return u + v; };
-    auto larger = [](double u, double v) { return most_of(u, v); };
-    sum = wave64(sum, plus);
-    if (Q8) most = wave64(most, larger);
+    if (Q8 && bad != bad) most = __builtin_inf();
+    sum = wave64(sum, [](double u, double v) { return u + v; });
+    if (Q8) most = wave64(most, [](double u, double v) { return __builtin_fmax(u, v); });
     if (NW > 1) {
         if (lane == 0) { s_sum[wave] = sum; s_most[wave] = most; }
         __syncthreads();
-        sum = 0.0; most = 0.0;
-        #pragma unroll
-        for (int w = 0; w < NW; ++w) { sum += s_sum[w]; if (Q8) most = most_of(most, s_most[w]); }
+        if (Q8) {
+            #pragma unroll
+            for (int w = 0; w < NW; ++w) most = __builtin_fmax(most, s_most[w]);
+        }
+        if (!Q8 || wave == 0) {
+            sum = 0.0;
+            #pragma unroll
+            for (int w = 0; w < NW; ++w) sum += s_sum[w];
+        }
     }
-    const double rstd = 1.0 / sqrt(sum / a.cols + (double)a.eps);
     const bool fine = most > 0.0 && most < __builtin_inf();
-    const double inv = fine ? 127.0 / most : 0.0;
-    const float rs = (float)rstd;
-    if (Q8 && tid == 0) a.scale[row] = fine ? (float)(most * rstd / 127.0) : (most == 0.0 ? 0.f : __builtin_nanf(""));
+    const double inv = Q8 && fine ? 127.0 / most : 0.0;
+    float rs = 0.f;
+    if (!Q8) rs = (float)(1.0 / sqrt(sum / a.cols + (double)a.eps));
+    else if (tid == 0)                                   // the only use of it: the codes do not depend on the sum
+        a.scale[row] = fine ? (float)(most / sqrt(sum / a.cols + (double)a.eps) / 127.0) : (most == 0.0 ? 0.f : __builtin_nanf(""));
     auto finish = [&](int c, const H (&hw)[8], const int* at) {
         const int n = a.cols - c;
         if constexpr (Q8) {
