@@ -481,20 +481,11 @@ int launched() {
     return PIVOT_OK;
 }
 
-int reserve(const void* k, size_t smem) {
-    if (smem > 64 * 1024 && hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess) {
-        (void)hipGetLastError();
-        set_error("cannot reserve %zu bytes of LDS", smem);
-        return PIVOT_E_HIP;
-    }
-    return PIVOT_OK;
-}
-
 template <int GPK, bool ZP>
 int up_go(const MoeLaunch& L, int vec) {
     auto go = [&](auto k, int rs, int w) {
         const size_t smem = std::max((size_t)w * 2 * L.tokens * QElem<false>::kRow, (size_t)w * 1024 * rs);
-        const int rc = reserve(reinterpret_cast<const void*>(k), smem);
+        const int rc = reserve_lds(reinterpret_cast<const void*>(k), smem);
         if (rc != PIVOT_OK) return rc;
         hipLaunchKernelGGL(k, dim3(L.nstrips[0] / rs, std::min(L.E, L.tokens * L.top_k)), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L, vec);
         return launched();
@@ -514,7 +505,7 @@ int down_go(const MoeLaunch& L, int) {
         int parts = 1;
         while (parts < kMoeMaxParts && L.nstrips[1] * parts < 256 && units >= 4 * w * parts) parts *= 2;
         const size_t smem = (size_t)w * rows * QElem<false>::kRow;      // more than the sums'
-        const int rc = reserve(reinterpret_cast<const void*>(k), smem);
+        const int rc = reserve_lds(reinterpret_cast<const void*>(k), smem);
         if (rc != PIVOT_OK) return rc;
         hipLaunchKernelGGL(k, dim3(L.nstrips[1], parts), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(L.stream), L);
         return launched();

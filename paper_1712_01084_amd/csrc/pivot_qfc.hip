@@ -1,7 +1,35 @@
 // Layers with 4-bit weights: laying the weights out on the device, and the choice of a launch.
+#include <mutex>
+#include <unordered_map>
+
 #include "pivot_qfc_kernel.h"
 
 namespace pivot {
+
+int reserve_lds(const void* kernel, size_t bytes) {
+    constexpr int kMost = 144 * 1024;                            // leaves 16 KB of a compute unit for what kernels declare
+    if (bytes <= 64 * 1024) return PIVOT_OK;
+    static std::mutex lock;
+    static std::unordered_map<const void*, uint64_t> done;     // a bit per device
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e == hipSuccess && bytes <= kMost) {
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+        std::lock_guard<std::mutex> g(lock);
+        try {
+            uint64_t& known = done[kernel];
+            if (known & bit) return PIVOT_OK;
+            e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMost);
+            if (e == hipSuccess) { known |= bit; return PIVOT_OK; }
+        } catch (...) {                                          // no memory to note it in
+            e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+            if (e == hipSuccess) return PIVOT_OK;
+        }
+    }
+    (void)hipGetLastError();
+    set_error("cannot reserve %zu bytes of LDS", bytes);
+    return PIVOT_E_HIP;
+}
 
 // One wavefront per unit: lane l gathers the 32 codes of row l % 16 that it will multiply, and the unit's scales.
 __global__ void __launch_bounds__(64) qfc_pack_kernel(u32x4* codes, uint16_t* scales, uint8_t* zeros, const uint8_t* raw_codes,

@@ -165,14 +165,8 @@ inline size_t qfc_smem(const QfcForm& f, int batch, int row) {
 
 template <typename K>
 inline int qfc_go(K k, const QfcArgs& a, int grid, int w, size_t smem, void* stream) {
-    if (smem > 64 * 1024) {
-        // asked for on every call: the attribute belongs to the device that is current
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(k), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess) {
-            (void)hipGetLastError();
-            set_error("cannot reserve %zu bytes of LDS", smem);
-            return PIVOT_E_HIP;
-        }
-    }
+    const int rc = reserve_lds(reinterpret_cast<const void*>(k), smem);
+    if (rc != PIVOT_OK) return rc;
     hipLaunchKernelGGL(k, dim3(grid), dim3(w * 64), smem, reinterpret_cast<hipStream_t>(stream), a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }

@@ -86,6 +86,9 @@ struct NormLaunch {
 };
 int launch_norm(const NormLaunch& L);
 
+// Lets `kernel` be launched on the current device with more than 64 KB of LDS (asked of the runtime once per device: 1 us).
+int reserve_lds(const void* kernel, size_t bytes);
+
 // ---- mixture of experts
 constexpr int kMoeMaxTokens = 16, kMoeMaxExperts = 256, kMoeMaxTopK = 8;
 constexpr int kMoeMaxActive = kMoeMaxTokens * kMoeMaxTopK;

@@ -14,12 +14,14 @@ namespace {
 
 struct DeviceGuard {
     int prev = -1;
-    bool ok = true;
+    bool ok = true, changed = false;
     explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) { ok = false; return; }
-        if (prev != dev && hipSetDevice(dev) != hipSuccess) ok = false;
+        if (hipGetDevice(&prev) != hipSuccess) { (void)hipGetLastError(); ok = false; return; }
+        if (prev == dev) return;
+        if (hipSetDevice(dev) == hipSuccess) changed = true;
+        else { (void)hipGetLastError(); ok = false; }
     }
-    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
+    ~DeviceGuard() { if (changed) (void)hipSetDevice(prev); }
 };
 
 struct DeviceMemory {       // freed unless released
@@ -195,6 +197,8 @@ int pivot_qfc_run(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, in
     const size_t nt = qfc_ticket_bytes(h), np = qfc_partial_bytes(h, batch);
     int rc = need_workspace(ws_dev, ws_bytes, nt + np + qfc_copy_bytes(h, batch));
     if (rc != PIVOT_OK) return rc;
+    DeviceGuard g(plan->device);
+    if (!g.ok) { set_error("cannot select device %d", plan->device); return PIVOT_E_HIP; }
     QfcLaunch L{};
     L.h = &h; L.d = &plan->dev; L.x = x_dev; L.xtype = xtype; L.ldx = ldx; L.xscale = xscale_dev; L.block_order = flags & PIVOT_QFC_X_BLOCK_ORDER;
     L.y = y_dev; L.ldy = ldy; L.batch = batch; L.tickets = static_cast<uint32_t*>(ws_dev);
@@ -242,6 +246,9 @@ int pivot_norm_run(const pivot_norm_args* args, void* stream) {
         if (a.order->host.d.K != a.cols) { set_error("the plan takes %d columns, not %d", a.order->host.d.K, a.cols); return PIVOT_E_SHAPE; }
         if (!a.order->host.identity_cols) order = a.order->dev.invpcol;
     }
+    if (!a.order) return run_norm(a, order, stream);
+    DeviceGuard g(a.order->device);
+    if (!g.ok) { set_error("cannot select device %d", a.order->device); return PIVOT_E_HIP; }
     return run_norm(a, order, stream);
 }
 
@@ -348,6 +355,8 @@ int pivot_moe_run(const pivot_moe_plan_t* plan, const void* x_dev, int xtype, in
     const MoeScratch s = moe_scratch(plan, tokens);
     int rc = need_workspace(ws_dev, ws_bytes, s.total);
     if (rc != PIVOT_OK) return rc;
+    DeviceGuard g(plan->device);
+    if (!g.ok) { set_error("cannot select device %d", plan->device); return PIVOT_E_HIP; }
     char* ws = static_cast<char*>(ws_dev);
     MoeLaunch L{};
     L.x = x_dev; L.ldx = ldx;
