@@ -82,7 +82,9 @@ __device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& 
             for (int w = 0; w < W; ++w) s += red[w * N + e];
         }
         if (Q8) s *= kQ8Factor<ZP> * a.xscale[n];
-        if (dst >= 0) a.y[n * a.ldy + dst] = apply_act(s + a.bias[row], a.act);
+        s += a.bias[row];
+        if (a.act == PIVOT_ACT_RELU && s < 0.f) s = 0.f;      // (a NaN stays one)
+        if (dst >= 0) a.y[n * a.ldy + dst] = s;
     }
 }
 

@@ -234,6 +234,7 @@ int pivot_norm_run(const pivot_norm_args* args, void* stream) {
     if (a.otype != PIVOT_Q8 && a.scale) { set_error("scale is for PIVOT_Q8"); return PIVOT_E_UNSUPPORTED; }
     if (!(a.eps >= 0.f) || std::isinf(a.eps)) { set_error("eps must be finite and not negative"); return PIVOT_E_SHAPE; }
     if (a.ldx < a.cols || a.ldo < a.cols || (a.res && a.ldr < a.cols) || (a.res_out && a.ldro < a.cols)) { set_error("a row stride is smaller than cols"); return PIVOT_E_SHAPE; }
+    if (a.out == a.x || a.out == a.res || a.out == a.res_out || (a.res_out && a.res_out == a.x)) { set_error("out and res_out must not be x, nor out the residual"); return PIVOT_E_UNSUPPORTED; }
     if (a.res_out == a.res && a.res && a.ldro != a.ldr) { set_error("res in place needs ldro = ldr"); return PIVOT_E_SHAPE; }
     if (!aligned_to(a.x, type_size(a.xtype)) || (a.res && !aligned_to(a.res, type_size(a.rtype))) || (a.res_out && !aligned_to(a.res_out, type_size(a.rtype))) ||
         !aligned_to(a.weight, 4) || !aligned_to(a.out, type_size(a.otype)) || !aligned_to(a.scale, 4)) {

@@ -59,6 +59,9 @@ CASES = [  # E, k, D, F, tile, kept, zeros, perm, renorm, router
     (256, 8, 96, 40, (16, 32, 64), 0.7, False, True, True, np.float32),
     (5, 3, 1000, 700, (32, 64, 32), 0.4, True, True, True, np.float16),
     (70, 8, 520, 130, (64, 32, 128), 0.5, False, False, False, np.float16),
+    (3, 2, 64, 4096, (32, 64, 64), 1.0, True, False, True, np.float16),          # two strips per work item, outputs in parts
+    (3, 2, 60, 4100, (64, 32, 32), 0.9, False, True, True, np.float16),          # the same, gathered
+    (4, 2, 64, 32, (16, 32, 32), 0.0, False, False, True, np.float16),           # nothing but biases
 ]
 
 
@@ -81,10 +84,31 @@ def test_against_the_definition(case):
 
 
 def test_tokens_that_all_choose_the_same_experts():
-    m = Layer(1, 12, 2, 64, 48, perm=True)
+    m = Layer(1, 12, 2, 64, 300, perm=True)
     try:
-        x = np.repeat(m.rng.normal(size=(1, 64)), 16, 0).astype(np.float16)
-        m.check(x.astype(np.float64), *m.run(torch.from_numpy(x).cuda(), 16))
+        for tokens in (7, 8, 16):
+            x = np.repeat(m.rng.normal(size=(1, 64)), tokens, 0).astype(np.float16)
+            m.check(x.astype(np.float64), *m.run(torch.from_numpy(x).cuda(), tokens))
+    finally:
+        m.close()
+
+
+def test_two_streams_at_once():
+    m = Layer(12, 16, 2, 128, 200, perm=True)
+    try:
+        jobs = []
+        for k in range(2):
+            x = m.rng.normal(size=(5, 128)).astype(np.float16)
+            jobs.append((torch.cuda.Stream(), x, torch.from_numpy(x).cuda(), G.workspace(B.pivot_moe_workspace_bytes(m.p, 5))))
+        torch.cuda.synchronize()
+        outs = [None, None]
+        for _ in range(20):
+            for k, (s, x, xd, ws) in enumerate(jobs):
+                with torch.cuda.stream(s):
+                    outs[k] = m.run(xd, 5, ws=ws)
+        torch.cuda.synchronize()
+        for (s, x, xd, ws), out in zip(jobs, outs):
+            m.check(x.astype(np.float64), *out)
     finally:
         m.close()
 

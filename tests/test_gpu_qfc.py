@@ -63,6 +63,67 @@ def test_exact_sums(shape, zeros, xtype, block):
         B.pivot_qfc_plan_destroy(p)
 
 
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True)])
+@pytest.mark.parametrize("perm", [False, True])
+@pytest.mark.parametrize("xtype", [B.PIVOT_F16, B.PIVOT_Q8])
+def test_every_form(group, zeros, perm, xtype):
+    """Sizes at which two strips make a work item, x is copied first in either order, or is read as it lies."""
+    rng = np.random.default_rng(group + perm)
+    seen = set()
+    for M, K, bh in ((16384, 600, 32), (8200, 664, 64), (4096, 700, 16)):
+        L = U.layer(rng, M, K, bh, max(32, group), group, kept=0.9, zeros=zeros, perm=perm, whole=True, act=1)
+        p = U.plan(L)
+        try:
+            x, xd, sd = inputs(rng, L, 64, xtype, False)
+            want = Q.qfc(L, x)[0].astype(np.float32)
+            for batch in (1, 4, 7, 16, 24, 64):
+                seen.add(B.pivot_qfc_kernel_name(p, xtype, batch))
+                y = run(p, L, xd, sd, batch, xtype, False).cpu().numpy()
+                assert np.array_equal(y, want[:batch]), "%dx%d batch %d" % (M, K, batch)
+        finally:
+            B.pivot_qfc_plan_destroy(p)
+    forms = {(n[:n.index("<")], tuple(n.rstrip(">").split(", ")[3:])) for n in seen}                     # without the types
+    assert len(forms) >= 6, sorted(forms)
+
+
+def test_the_longest_rows_and_layers_without_tiles():
+    rng = np.random.default_rng(65535)
+    for M, K, kept in ((40, 65535, 1.0), (100, 300, 0.0)):
+        L = U.layer(rng, M, K, 32, 128, 128, kept=kept, zeros=True, perm=True, whole=True)
+        L["scales"][:] = 0.5                                   # sums of up to 65535 * 15 * 9 / 2 stay exact
+        p = U.plan(L)
+        try:
+            for batch in (1, 3, 20):
+                for xtype in (B.PIVOT_F16, B.PIVOT_Q8):
+                    x, xd, sd = inputs(rng, L, batch, xtype, False)
+                    y = run(p, L, xd, sd, batch, xtype, False).cpu().numpy()
+                    assert np.array_equal(y, Q.qfc(L, x)[0].astype(np.float32))
+        finally:
+            B.pivot_qfc_plan_destroy(p)
+
+
+def test_two_streams_at_once():
+    rng = np.random.default_rng(12)
+    L = U.layer(rng, 1000, 2000, 32, 64, 64, kept=0.8, zeros=True, perm=True, whole=True)
+    p = U.plan(L, chunk_blocks=3)
+    try:
+        jobs = []
+        for k in range(2):
+            x, xd, sd = inputs(rng, L, 9, B.PIVOT_F16, False)
+            jobs.append((torch.cuda.Stream(), xd, Q.qfc(L, x)[0].astype(np.float32), G.workspace(B.pivot_qfc_workspace_bytes(p, 9)),
+                         torch.zeros(9, 1000, device="cuda")))
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for s, xd, _, ws, y in jobs:
+                with torch.cuda.stream(s):
+                    run(p, L, xd, None, 9, B.PIVOT_F16, False, ws=ws, y=y)
+        torch.cuda.synchronize()
+        for _, _, want, _, y in jobs:
+            assert np.array_equal(y.cpu().numpy(), want)
+    finally:
+        B.pivot_qfc_plan_destroy(p)
+
+
 @pytest.mark.parametrize("chunk_blocks", [1, 2, 5])
 @pytest.mark.parametrize("bh", [16, 64])
 def test_block_rows_in_pieces_on_one_workspace(chunk_blocks, bh):
@@ -146,6 +207,13 @@ def test_numbers_at_the_edges():
         assert (y[1:, lost] == 0).all()
         rest = np.setdiff1d(np.arange(64), lost)
         assert np.isposinf(y[1, rest]).all() and np.isnan(y[2, rest]).all()
+    finally:
+        B.pivot_qfc_plan_destroy(p)
+    p = U.plan(dict(L, act=1))
+    try:
+        x[1] *= -1
+        y = run(p, dict(L, act=1), torch.from_numpy(x).cuda(), None, 3, B.PIVOT_F16, False).cpu().numpy()
+        assert (y[1] == 0).all() and np.isnan(y[2, rest]).all()              # the activation keeps a NaN
     finally:
         B.pivot_qfc_plan_destroy(p)
 

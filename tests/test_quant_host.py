@@ -76,7 +76,7 @@ def test_runs_that_are_refused():
     try:
         _refused(B.PIVOT_E_NO_DEVICE, B.pivot_qfc_run, p, 1024, B.PIVOT_F16, 100, None, 1024, 40, 1, None, 0)
         _refused(B.PIVOT_E_NULL, B.pivot_qfc_run, None, 1024, B.PIVOT_F16, 100, None, 1024, 40, 1, None, 0)
-        _refused(B.PIVOT_E_NO_DEVICE, B.pivot_norm_run, 1024, B.PIVOT_F32, 100, 1024, B.PIVOT_F32, 100, 1, 100, order=p)
+        _refused(B.PIVOT_E_NO_DEVICE, B.pivot_norm_run, 1024, B.PIVOT_F32, 100, 4096, B.PIVOT_F32, 100, 1, 100, order=p)
         assert B.pivot_qfc_kernel_name(p, B.PIVOT_F16, 1).startswith("pivot::qfc_rows_kernel<false")
         assert B.pivot_qfc_kernel_name(p, B.PIVOT_Q8, 64).startswith("pivot::qfc_frag_kernel<true")
         _refused(B.PIVOT_E_SHAPE, B.pivot_qfc_kernel_name, p, B.PIVOT_F16, 65)
@@ -98,6 +98,9 @@ def test_runs_that_are_refused():
                        (B.PIVOT_E_UNSUPPORTED, (1024, F32, 8, 4096, F32, 8, 1, 8), dict(n, rtype=Q8)),
                        (B.PIVOT_E_SHAPE, (1024, F32, 8, 4096, F32, 8, 1, 8), dict(eps=-1.0)),
                        (B.PIVOT_E_SHAPE, (1024, F32, 8, 4096, F32, 8, 1, 8), dict(eps=float("nan"))),
+                       (B.PIVOT_E_UNSUPPORTED, (1024, F32, 8, 1024, F32, 8, 1, 8), {}), (B.PIVOT_E_UNSUPPORTED, (1024, F32, 8, 2048, F32, 8, 1, 8), n),
+                       (B.PIVOT_E_UNSUPPORTED, (1024, F32, 8, 4096, F32, 8, 1, 8), dict(n, res_out_ptr=4096, ldro=8)),
+                       (B.PIVOT_E_UNSUPPORTED, (1024, F32, 8, 4096, F32, 8, 1, 8), dict(n, res_out_ptr=1024, ldro=8)),
                        (B.PIVOT_E_SHAPE, (1025, F32, 8, 4096, F32, 8, 1, 8), {})):
         _refused(code, B.pivot_norm_run, *a, **k)
 
