@@ -453,7 +453,7 @@ typedef struct pivot_qfc_plan pivot_qfc_plan_t;
 /* The schedule of a plan (valid until the plan is destroyed).  The kept tiles of a block row, side by side, are cut
  * into blocks of 128 columns (the last one filled up); `pieces` gives for each bw columns of a block the first
  * block-space column they come from, or -1.  `chunks`: (block row, first block, end, first slot of the row, pieces
- * of the row, slot, 0, 0), longest first.  The sums of a block row in several pieces are added in ascending slot order. */
+ * of the row, slot, the row's first block, its blocks), longest first.  The sums of a block row in several pieces are added in ascending slot order. */
 typedef struct pivot_qfc_view {
     int32_t M, K, bh, bw, group, act, nbr, nbc, M_pad, K_pad, T, blocks, chunk_blocks, nchunks, groups_per_block;
     const int32_t* row_ptr;    /* [nbr+1] kept tiles before block row i */

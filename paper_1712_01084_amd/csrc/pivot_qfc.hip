@@ -138,11 +138,11 @@ int launch_qfc(const QfcLaunch& L, std::string* describe) {
     }
     const QfcDev& d = *L.d;
     QfcArgs a{};
-    a.codes = reinterpret_cast<const u32x4*>(d.codes); a.scales = d.scales; a.zeros = d.zeros; a.chunks = d.chunks; a.kb_ptr = d.kb_ptr; a.pieces = d.pieces;
+    a.codes = reinterpret_cast<const u32x4*>(d.codes); a.scales = d.scales; a.zeros = d.zeros; a.chunks = d.chunks; a.pieces = d.pieces;
     a.prow = d.prow_pad; a.bias = d.bias_p; a.xscale = L.xscale;
     a.x = QSource{L.x, L.ldx, gathered ? d.pcol_pad : nullptr, h.d.K, vec};
     a.y = L.y; a.ldy = L.ldy; a.partials = L.partials; a.tickets = L.tickets;
-    a.bh = h.d.bh; a.bw_log2 = h.d.bw == 32 ? 5 : (h.d.bw == 64 ? 6 : 7); a.batch = L.batch; a.act = h.d.act; a.zero_chunk = h.K_pad / 32; a.whole = h.whole ? h.max_kb : 0;
+    a.bh = h.d.bh; a.bw_log2 = h.d.bw == 32 ? 5 : (h.d.bw == 64 ? 6 : 7); a.batch = L.batch; a.act = h.d.act; a.zero_chunk = h.K_pad / 32; a.whole = h.whole ? h.max_kb : 0; a.row_items = h.nchunks == h.nbr;
     if (copy) {
         const int blocks = ((h.K_pad / 32 + 1) * L.batch * 4 + 255) / 256;
         hipStream_t st = reinterpret_cast<hipStream_t>(L.stream);

@@ -9,11 +9,11 @@
 namespace pivot {
 
 struct QfcArgs {
-    const u32x4* codes; const uint16_t* scales; const uint8_t* zeros; const int32_t* chunks; const int32_t* kb_ptr; const int32_t* pieces;
+    const u32x4* codes; const uint16_t* scales; const uint8_t* zeros; const int32_t* chunks; const int32_t* pieces;
     const int32_t* prow; const float* bias; const float* xscale;
     QSource x;              // rows form: the rows; fragment form: x.x alone
     float* y; long long ldy; float* partials; uint32_t* tickets;
-    int bh, bw_log2, batch, act, zero_chunk, whole;   // whole > 0: every tile is kept, so many blocks in each block row
+    int bh, bw_log2, batch, act, zero_chunk, whole, row_items;   // whole > 0: every tile is kept, so many blocks in each block row; row_items: items are whole block rows
 };
 
 // A work item: RS strips of a block row times a piece of its columns; blockIdx.x = piece * (strips / RS) + strip group.
@@ -24,10 +24,12 @@ struct QfcItem {
     __device__ __forceinline__ explicit QfcItem(const QfcArgs& a) {
         const int groups = a.bh / (kQStrip * RS), piece = blockIdx.x / groups;
         sg = blockIdx.x % groups;
-        const int32_t* ch = a.chunks + 8 * piece;
-        br = ch[0]; kb0 = ch[1]; kb1 = ch[2]; first = ch[3]; parts = ch[4]; slot = ch[5];
-        rowkb = a.whole ? br * a.whole : a.kb_ptr[br];
-        nkb = a.whole ? a.whole : a.kb_ptr[br + 1] - rowkb;
+        if (a.whole && a.row_items) {                    // every row as long as the others and in one piece: nothing to look up
+            br = first = slot = piece; parts = 1; nkb = a.whole; rowkb = br * nkb; kb0 = rowkb; kb1 = rowkb + nkb;
+        } else {
+            const int32_t* ch = a.chunks + 8 * piece;
+            br = ch[0]; kb0 = ch[1]; kb1 = ch[2]; first = ch[3]; parts = ch[4]; slot = ch[5]; rowkb = ch[6]; nkb = ch[7];
+        }
         unit0 = (size_t)rowkb * (a.bh / kQStrip) + (size_t)(sg * RS) * nkb;      // units of a block row: strip-major
         kb0 -= rowkb;
         kb1 -= rowkb;
@@ -36,8 +38,16 @@ struct QfcItem {
 
 // Sums of the wavefronts, through LDS (W * 16 RS * 16 NT floats at `red`); pieces of a row through memory; bias,
 // activation and the scatter through prow.
+// What the end of an item needs of memory, asked for at its beginning: where this thread's (first) output goes, its bias.
+struct QfcEnd { int dst; float bias; };
+template <int RS>
+__device__ __forceinline__ QfcEnd qfc_end(const QfcArgs& a, const QfcItem<RS>& it) {
+    const int row = it.br * a.bh + it.sg * 16 * RS + threadIdx.x % (16 * RS);
+    return QfcEnd{a.prow[row], a.bias[row]};
+}
+
 template <bool Q8, bool ZP, int NT, int RS, int W>
-__device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& it, const f32x4 (&acc)[RS][NT], float* red) {
+__device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& it, const QfcEnd& end, const f32x4 (&acc)[RS][NT], float* red) {
     constexpr int N = 16 * RS * 16 * NT;
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = q_wave();
@@ -73,7 +83,7 @@ __device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& 
         if (!s_last) return;
     }
     for (int e = tid; e < n_out; e += W * 64) {
-        const int row = it.br * a.bh + it.sg * 16 * RS + e % (16 * RS), n = e / (16 * RS), dst = a.prow[row];
+        const int n = e / (16 * RS);                      // (a thread's outputs are all of one row: 16 * RS divides W * 64)
         float s = 0.f;
         if (it.parts > 1) {
             for (int q = 0; q < it.parts; ++q) s += agent_load(a.partials + (it.first + q) * slot_len + strip_off + e);
@@ -82,9 +92,9 @@ __device__ __forceinline__ void qfc_finish(const QfcArgs& a, const QfcItem<RS>& 
             for (int w = 0; w < W; ++w) s += red[w * N + e];
         }
         if (Q8) s *= kQ8Factor<ZP> * a.xscale[n];
-        s += a.bias[row];
+        s += end.bias;
         if (a.act == PIVOT_ACT_RELU && s < 0.f) s = 0.f;      // (a NaN stays one)
-        if (dst >= 0) a.y[n * a.ldy + dst] = s;
+        if (end.dst >= 0) a.y[n * a.ldy + end.dst] = s;
     }
 }
 
@@ -99,10 +109,11 @@ __global__ void __launch_bounds__(W * 64, 4) qfc_rows_kernel(QfcArgs a) {
     extern __shared__ __align__(16) char smem[];
     const int wave = q_wave();
     const QfcItem<RS> it(a);
+    const QfcEnd end = qfc_end(a, it);
     f32x4 acc[RS][1] = {};
     const QWalk k{a.codes, a.scales, a.zeros, a.whole ? nullptr : a.pieces + ((size_t)it.rowkb << (7 - a.bw_log2)), it.unit0, it.nkb, it.kb0 + wave, it.kb1, a.bw_log2};
     q_walk_rows<Q8, GPK, ZP, RS, FAST, W>(k, a.x, a.batch, [](int n) { return n; }, smem + wave * (2 * a.batch * QElem<Q8>::kRow), acc);
-    qfc_finish<Q8, ZP, 1, RS, W>(a, it, acc, reinterpret_cast<float*>(smem));
+    qfc_finish<Q8, ZP, 1, RS, W>(a, it, end, acc, reinterpret_cast<float*>(smem));
 }
 
 // Fragment form: x lies in memory as the matrix instructions read it (qfc_gather_kernel), NT * 16 batch columns.  No LDS but
@@ -114,6 +125,7 @@ __global__ void __launch_bounds__(W * 64) qfc_frag_kernel(QfcArgs a) {
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, wave = q_wave();
     const QfcItem<RS> it(a);
+    const QfcEnd end = qfc_end(a, it);
     f32x4 acc[RS][NT] = {};
     int at[NT];                                           // this lane's place in a chunk
     #pragma unroll
@@ -161,7 +173,7 @@ __global__ void __launch_bounds__(W * 64) qfc_frag_kernel(QfcArgs a) {
             if (kb >= it.kb1) break;
         }
     }
-    qfc_finish<Q8, ZP, NT, RS, W>(a, it, acc, reinterpret_cast<float*>(smem));
+    qfc_finish<Q8, ZP, NT, RS, W>(a, it, end, acc, reinterpret_cast<float*>(smem));
 }
 
 // The form a call takes: rows (frag = 0) or fragment, column tiles, strips per item, rows form: whether x is read as

@@ -40,7 +40,7 @@ struct QfcHost {
     std::vector<int32_t> row_ptr, col_idx;
     std::vector<int32_t> kb_ptr;        // [nbr+1] blocks of 128 kept columns before block row i
     std::vector<int32_t> pieces;        // [KB * 128 / bw] first block-space column of each bw columns, -1 = none
-    std::vector<int32_t> chunks;        // [nchunks][8]: block row, first block, end, first slot of the row, pieces of the row, slot, 0, 0
+    std::vector<int32_t> chunks;        // [nchunks][8]: block row, first block, end, first slot of the row, pieces of the row, slot, the row's first block, its blocks
     std::vector<int32_t> prow_pad, pcol_pad, invprow, invpcol;
     std::vector<float>   bias_p;
     int strips() const { return d.bh / kQStrip; }

@@ -96,7 +96,7 @@ int build_qfc_host(const pivot_qfc_desc& d, const uint8_t* zeros, int64_t groups
     }
     std::stable_sort(cs.begin(), cs.end(), [](const Chunk& a, const Chunk& b) { return a.e - a.b > b.e - b.b; });
     h.nchunks = (int)cs.size();
-    for (const Chunk& c : cs) for (int v : {c.row, c.b, c.e, c.first, c.parts, c.slot, 0, 0}) h.chunks.push_back(v);
+    for (const Chunk& c : cs) for (int v : {c.row, c.b, c.e, c.first, c.parts, c.slot, h.kb_ptr[c.row], h.kb_ptr[c.row + 1] - h.kb_ptr[c.row]}) h.chunks.push_back(v);
     return PIVOT_OK;
 } catch (const std::bad_alloc&) {
     set_error("out of host memory");
