@@ -4,9 +4,9 @@
 //
 // TPR threads share a row, eight neighbouring columns each at a time, and keep weight * h in registers between the two
 // passes (sum of squares and largest weight * h, then the outputs); what of a row does not fit there is read a second
-// time.  8192x4096, residual and output fp16: 54 us = 5.0 TB/s, what a copy reaches; fp32 into 8 bits 81 us = 5.4; fp16 into 8
-// bits 62 us = 3.8, bound by the 64-bit operations.  One row of 4096: 3.2 us, 3.5 into 8 bits, 5.3 in block order: launch, one
-// trip, two reductions, stores.  Rows of up to 8192 columns are kept whole; 64x9203 fp32 into fp16 5.7 us.
+// time.  8192x4096, residual and output fp16: 54 us = 5.0 TB/s, what a copy reaches; fp32 into 8 bits 83 us = 5.2; fp16 into 8
+// bits 62 us = 3.8, bound by the 64-bit operations.  One row of 4096: 3.1 us, 3.6 into 8 bits, 5.4 in block order: launch, one
+// trip, two reductions, stores.  Rows of up to 16384 columns are kept whole; 64x9203 fp32 into fp16 5.3 us.
 // The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
 // 10^5 would fall to the other side of the middle between two.
 #include <type_traits>
@@ -21,22 +21,34 @@ namespace {
 typedef float    f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 typedef _Float16 f16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 
-// Eight neighbouring elements as floats, the first `n` of them real (the others 0).
-__device__ __forceinline__ void norm_load(const void* p, int type, long long at, int n, float (&v)[8]) {
+// Eight neighbouring elements as they lie in memory, the first `n` of them real (the others 0).  Loading and converting are
+// apart, so that no load of a row waits for another.
+struct NormRaw { u32x4 a, b; };
+__device__ __forceinline__ void norm_load(const void* p, int type, long long at, int n, NormRaw& r) {
+    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    const char* q = reinterpret_cast<const char*>(p) + at * (type == PIVOT_F32 ? 4 : 2);
     if (n >= 8) {
-        if (type == PIVOT_F32) {
-            const f32x4_any a = gload<f32x4_any>((const float*)p + at), b = gload<f32x4_any>((const float*)p + at + 4);
-            #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
-        } else {
-            const f16x8_any a = gload<f16x8_any>((const _Float16*)p + at);
-            #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = (float)a[i];
-        }
+        r.a = gload<u32x4_any>(q);
+        if (type == PIVOT_F32) r.b = gload<u32x4_any>(q + 16);
         return;
     }
     #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i >= n ? 0.f : (type == PIVOT_F32 ? gload<float>((const float*)p + at + i) : (float)gload<_Float16>((const _Float16*)p + at + i));
+    for (int i = 0; i < 8; ++i) {
+        uint32_t v = 0;
+        if (i < n) v = type == PIVOT_F32 ? gload<uint32_t>(q + 4 * i) : gload<uint16_t>(q + 2 * i);
+        if (type == PIVOT_F32) { if (i < 4) r.a[i & 3] = v; else r.b[i & 3] = v; }
+        else r.a[i >> 1] = i & 1 ? r.a[i >> 1] | v << 16 : v;
+    }
+}
+__device__ __forceinline__ void norm_floats(const NormRaw& r, int type, float (&v)[8]) {
+    if (type == PIVOT_F32) {
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_bit_cast(float, (uint32_t)(i < 4 ? r.a[i & 3] : r.b[i & 3]));
+    } else {
+        const f16x8 h = __builtin_bit_cast(f16x8, r.a);
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+    }
 }
 
 __device__ __forceinline__ void norm_store(void* p, int type, long long at, int n, const float (&v)[8]) {
@@ -115,27 +127,27 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
             #pragma unroll
             for (int i = 0; i < 8; ++i) { const int c = (tid + k * TPR) * 8 + i; place[k][i] = c < a.cols ? gload<int>(a.order + c) : 0; }
 
-    struct Piece { float x[8], r[8], w[8]; };
+    struct Piece { NormRaw x, r, w; };
     auto fetch = [&](int c, Piece& p) {
         const int n = a.cols - c;
         norm_load(a.x, a.xtype, xo + c, n, p.x);
         if (a.res) norm_load(a.res, a.rtype, ro + c, n, p.r);
-        else
-            #pragma unroll
-            for (int i = 0; i < 8; ++i) p.r[i] = 0.f;
         if (a.weight) norm_load(a.weight, PIVOT_F32, c, n, p.w);
-        else
-            #pragma unroll
-            for (int i = 0; i < 8; ++i) p.w[i] = 1.f;
     };
     double sum = 0.0, most = 0.0;
     float bad = 0.f;                                    // NaN once anything is infinite or NaN
     // weight * h of a piece; the sums on the first pass, what goes back to the residual on the last one
     auto combine = [&](int c, const Piece& p, H (&hw)[8], bool first, bool last) {
-        float back[8];
+        float back[8], px[8], pr[8] = {}, pw[8];
+        norm_floats(p.x, a.xtype, px);
+        if (a.res) norm_floats(p.r, a.rtype, pr);
+        if (a.weight) norm_floats(p.w, PIVOT_F32, pw);
+        else
+            #pragma unroll
+            for (int i = 0; i < 8; ++i) pw[i] = 1.f;
         #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float x = p.x[i], r = p.r[i], w = p.w[i];
+            const float x = px[i], r = pr[i], w = pw[i];
             const H h = (H)x + (H)r;
             back[i] = x + r;
             hw[i] = h * (H)w;
