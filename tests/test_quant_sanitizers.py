@@ -17,7 +17,7 @@ def test_plan_builder_under_asan_ubsan(tmp_path):
     exe = str(tmp_path / "quant_sanitize")
     cmd = [gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, os.path.join(ROOT, "tests", "quant_sanitize_driver.cpp"),
-           os.path.join(CSRC, "pivot_quant_plan.cpp"), os.path.join(CSRC, "pivot_plan.cpp"), "-o", exe]
+           os.path.join(CSRC, "pivot_quant_plan.cpp"), "-o", exe]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0 and "sanitize" in r.stdout and "cannot find" in r.stdout:
         pytest.skip("sanitizer runtime not installed")
