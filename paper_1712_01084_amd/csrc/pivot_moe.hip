@@ -360,10 +360,10 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
     constexpr int NX = 3;
     struct Turn { QUnit<GPK, ZP> u[P][1]; u32x4 v[NX]; int act[P], kb[P], mask[P], off[P + 1]; };
     const int c = 8 * (lane & 15), in = c & ((1 << bw_log2) - 1), slot = lane >> 4;
-    auto column = [&](int act, int kb) {                // where this lane's columns of a block begin, F and more: nowhere
+    auto column = [&](int act, int kb) {                // where this lane's columns of a block begin, F_pad and more: nowhere
         const int32_t* pieces = s_ex[act].pieces;
         const int piece = pieces ? gload<int>(pieces + (kb << (7 - bw_log2)) + (c >> bw_log2)) : (kb << 7) + c - in;
-        return piece < 0 ? a.F : piece + in;
+        return piece < 0 ? a.F_pad : piece + in;
     };
     auto values = [&](int act, int r, int ntok, int col) -> u32x4 {
         const int plane = r >= ntok, m = r - plane * ntok;
