@@ -124,8 +124,11 @@ def moe(x, router, bias, gate_up, down, top_k, renormalise):
         g, u, dg, du = z[:, 0::2], z[:, 1::2], dz[:, 0::2], dz[:, 1::2]
         silu = g / (1.0 + np.exp(-g))
         h = silu * u
-        # the slope of silu is below 1.1; an exponential, a sum, a division and a product; value and remainder keep 22 bits
-        dh = 1.1 * dg * np.abs(u) + np.abs(silu) * du + dg * du * 1.1 + np.abs(h) * (8 * U + 2.0 ** -22) + 2.0 ** -35
+        # the slope of silu is below 1.1; an exponential, a sum, a division and a product, stored in fp32; as value and remainder
+        # in fp16 under a power of two by which the largest lies in [2^14, 2^15): half a step of each, 2^-11 * 2^-11, or half
+        # the remainder's subnormal step, 2^-25 / 2^11 beside 2^14
+        dh = (1.1 * dg * np.abs(u) + np.abs(silu) * du + dg * du * 1.1 + np.abs(h) * (8 * U + 2.0 ** -22) + 2.0 ** -149
+              + 2.0 ** -50 * np.abs(h).max(axis=1, keepdims=True))
         W, A = dense_natural(dn)
         b = np.zeros(D) if dn["bias"] is None else np.asarray(dn["bias"], dtype=np.float64)
         d = h @ W.T + b

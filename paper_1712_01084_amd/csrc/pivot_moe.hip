@@ -3,10 +3,9 @@
 //   router   one workgroup per expert: its logit for every token; the last one to arrive ranks them, takes the softmax and
 //            writes down which experts are in use, by which tokens
 //   up       one workgroup per expert in use and strip of 16 rows (8 gate rows and their 8 up rows): silu(gate) * up,
-//            stored in the block order of the expert's down layer as fp16 value and remainder times 2^11 (22 bits, so
-//            that this boundary costs the result nothing an fp32 sum would keep)
+//            stored in fp32, in the block order of the expert's down layer
 //   down     one workgroup per strip of 16 outputs: all experts in use, one after the other, their sums weighted and added
-//            in the accumulators.  The tokens are the columns of the matrix instruction in every expert, so no expert's
+//            in the accumulators.  The matrix instruction takes an activation as two fp16 numbers (see moe_down_kernel).  The tokens are the columns of the matrix instruction in every expert, so no expert's
 //            output is ever stored and nothing is added across workgroups
 //
 // The weights of an expert in use are read once, whatever the number of its tokens.
@@ -55,6 +54,14 @@ __device__ __forceinline__ float lane_of(float v, int l) {
 __device__ __forceinline__ float wave_max(float v) {
     v = dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
     return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
+}
+// ... of sixteen neighbouring lanes.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+    return dpp_max<0x140>(dpp_max<0x141>(dpp_max<0x4E>(dpp_max<0xB1>(v))));
 }
 __device__ __forceinline__ float wave_sum(float v) {
     v = group_sum<16>(v);
@@ -266,21 +273,11 @@ __global__ void __launch_bounds__(W * 64, 4) moe_up_kernel(MoeLaunch a, int vec)
     auto finish = [&](int m, int u, int to, int row, float g, float v) {
         #pragma unroll
         for (int w = 0; w < W; ++w) { g += red[w * N + m * 16 * RS + 2 * u]; v += red[w * N + m * 16 * RS + 2 * u + 1]; }
-        const float h = g / (1.f + expf(-g)) * v;
-        const _Float16 hi = (_Float16)h;
-        // what fp16 leaves of h, 2^11 times: again fp16; nothing where h is beyond the range
-        const _Float16 lo = fabsf((float)hi) < __builtin_inff() ? (_Float16)((h - (float)hi) * 2048.f) : (_Float16)0.f;
-        if (to >= 0) {
-            _Float16* out = reinterpret_cast<_Float16*>(a.h) + (size_t)row * a.F_pad + to;
-            out[0] = hi;
-            out[(size_t)T * a.top_k * a.F_pad] = lo;
-        }
+        if (to >= 0) a.h[(size_t)row * a.F_pad + to] = g / (1.f + expf(-g)) * v;
     };
     if (blockIdx.x == 0)                                 // the columns that fill up the down layer's last tile
-        for (int i = tid; i < 2 * ntok * (a.F_pad - a.F); i += W * 64) {
-            const int m = i / (2 * (a.F_pad - a.F)), r = i % (2 * (a.F_pad - a.F)), plane = r & 1;
-            a.h[((size_t)plane * T * a.top_k + act.hrow[m]) * a.F_pad + a.F + r / 2] = 0;
-        }
+        for (int i = tid; i < ntok * (a.F_pad - a.F); i += W * 64)
+            a.h[(size_t)act.hrow[i / (a.F_pad - a.F)] * a.F_pad + a.F + i % (a.F_pad - a.F)] = 0.f;
     if (em < ntok) finish(em, eu, dst, hrow, bg, bu);
     for (int i = tid + W * 64; i < 8 * RS * ntok; i += W * 64) {
         const int m = i / (8 * RS), u = i % (8 * RS);
@@ -292,6 +289,13 @@ __global__ void __launch_bounds__(W * 64, 4) moe_up_kernel(MoeLaunch a, int vec)
 // gridDim.y workgroups take in turn, P at a time.  Sixteen wavefronts share what a workgroup looks up first, and most strips
 // need no hand-over (four wavefronts and parts in their place: 41.5 and 115 us for the layers above where this takes 39.6 and
 // 91).  NT = 2: values and remainders of h are two column tiles; NT = 1 (up to 8 tokens): columns 0-7 and 8-15 of one.
+//
+// A token's activations under a unit are staged by the sixteen lanes that load them as 2^s h = value + remainder / 2^11, both
+// fp16, s such that the largest of the unit's 128 lies in [2^14, 2^15); 2^-s multiplies the unit's sums.  Value and remainder
+// leave 2^-22 of an activation, or 2^-50 of the largest one (the remainder's last subnormal place) where that is more: less
+// than the 2^-23 that every addition of an fp32 sum of the products may cost, whatever the size of the activations.  A single
+// fp16 would leave 2^-11.
+//
 // rows that a wavefront stages: at least the values and remainders of all tokens in one unit
 template <int NT> constexpr int kDownRows = 16 * NT;
 template <int GPK, bool ZP, int NT, int W>
@@ -355,22 +359,39 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
     const int n = NT == 1 ? (lane & 7) : (lane & 15), second = NT == 1 ? (lane >> 3) & 1 : 0;
     f32x4 total[NT] = {};
     int cur = 0;
-    // A turn: P units, their rows of h (values, then remainders, of each unit's tokens) as one list of which the first
-    // twelve are asked for ahead.  As in the rows form every load is issued whatever the sizes: past the end the last unit's.
-    constexpr int NX = 3;
-    struct Turn { QUnit<GPK, ZP> u[P][1]; u32x4 v[NX]; int act[P], kb[P], mask[P], off[P + 1]; };
+    // A turn: P units, the tokens of both as one list of which the first eight are asked for ahead.  As in the rows form every load is issued whatever the sizes: past the end the last unit's.
+    constexpr int NX = 2;
+    struct Turn { QUnit<GPK, ZP> u[P][1]; f32x4 v[NX][2]; int act[P], kb[P], mask[P], off[P + 1]; };
     const int c = 8 * (lane & 15), in = c & ((1 << bw_log2) - 1), slot = lane >> 4;
     auto column = [&](int act, int kb) {                // where this lane's columns of a block begin, F_pad and more: nowhere
         const int32_t* pieces = s_ex[act].pieces;
         const int piece = pieces ? gload<int>(pieces + (kb << (7 - bw_log2)) + (c >> bw_log2)) : (kb << 7) + c - in;
         return piece < 0 ? a.F_pad : piece + in;
     };
-    auto values = [&](int act, int r, int ntok, int col) -> u32x4 {
-        const int plane = r >= ntok, m = r - plane * ntok;
-        const uint16_t* row = a.h + ((size_t)plane * T * a.top_k + s_hrow[act][m]) * a.F_pad;
-        u32x4 v = gload<u32x4>(row + min(col, a.F_pad - 8));           // (columns between F and F_pad hold zeros)
-        if (col >= a.F_pad) v = u32x4{};
-        return v;
+    auto load = [&](int act, int m, int col, f32x4 (&v)[2]) {              // of token m of the expert's
+        const float* p = a.h + (size_t)s_hrow[act][m] * a.F_pad + min(col, a.F_pad - 8);   // (columns between F and F_pad hold zeros)
+        v[0] = gload<f32x4>(p);
+        v[1] = gload<f32x4>(p + 4);
+        if (col >= a.F_pad) v[0] = v[1] = f32x4{};
+    };
+    auto stage = [&](const f32x4 (&v)[2], char* row, int ntok) {           // the remainders: ntok rows on; behind the values: 2^-s
+        uint32_t most = 0;                              // as integers magnitudes are in order, infinities and NaNs last
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) { const float f = v[i >> 2][i & 3]; most = max(most, __builtin_bit_cast(uint32_t, f) & 0x7fffffffu); }
+        most = row16_max(most);
+        const bool odd = most >= 0x7f800000u;           // (the unit's sums are infinite or NaN: no remainders)
+        const int e = min(max((int)(most >> 23), 15), 254);                // 2^-s and 2^s are both normal numbers
+        const float up = __builtin_bit_cast(float, (uint32_t)(268 - e) << 23);     // 2^(141 - e), e - 127 the exponent
+        f16x8 hi, lo;
+        #pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float x = v[i >> 2][i & 3] * up;
+            hi[i] = (_Float16)x;
+            lo[i] = odd ? (_Float16)0.f : (_Float16)((x - (float)hi[i]) * 2048.f);
+        }
+        q_store8<false>(row, lane & 15, __builtin_bit_cast(u32x4, hi));
+        q_store8<false>(row + ntok * ROW, lane & 15, __builtin_bit_cast(u32x4, lo));
+        if ((lane & 15) == 0) *reinterpret_cast<float*>(row + 2 * kQBlk) = __builtin_bit_cast(float, (uint32_t)(e - 14) << 23);
     };
     auto fetch = [&](Turn& t, int u0) {
         t.off[0] = 0;
@@ -381,22 +402,21 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
             t.act[p] = __builtin_amdgcn_readfirstlane(cur);
             t.kb[p] = __builtin_amdgcn_readfirstlane(g - s_cum[cur]);
             t.mask[p] = u0 + p * step < units ? __builtin_amdgcn_readfirstlane(s_mask[cur]) : 0;
-            t.off[p + 1] = t.off[p] + 2 * __popc(t.mask[p]);
+            t.off[p + 1] = t.off[p] + __popc(t.mask[p]);
         }
-        int act[NX], at[NX], ntok[NX], col[NX];         // this lane's row of h in each place of the list
+        int act[NX], at[NX], col[NX];                   // this lane's token in each place of the list
         #pragma unroll
         for (int q = 0; q < NX; ++q) {
             const int i = max(0, min(slot + 4 * q, t.off[P] - 1));
             const bool first = i < t.off[1];
             act[q] = first ? t.act[0] : t.act[1];
             at[q] = first ? i : i - t.off[1];
-            ntok[q] = __popc(first ? t.mask[0] : t.mask[1]);
             col[q] = column(act[q], first ? t.kb[0] : t.kb[1]);
         }
         #pragma unroll
         for (int p = 0; p < P; ++p) t.u[p][0].load(s_ex[t.act[p]].codes, s_ex[t.act[p]].scales, s_ex[t.act[p]].zeros, t.kb[p], lane);
         #pragma unroll
-        for (int q = 0; q < NX; ++q) t.v[q] = values(act[q], at[q], ntok[q], col[q]);
+        for (int q = 0; q < NX; ++q) load(act[q], at[q], col[q], t.v[q]);
     };
     auto multiply_unit = [&](const Turn& t, int p, int at) {
         const int mask = t.mask[p], ntok = __popc(mask);
@@ -409,26 +429,34 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
         const QRows<false, NT> x{xs, nrow, lane};
         q_multiply<false, GPK, ZP, NT, 1>(t.u[p], x, part);
         // tokens that do not use the expert: what their column held is dropped
-        const float share = s_share[t.act[p]][n];
+        const float share = s_share[t.act[p]][n], down = *reinterpret_cast<const float*>(xs + (at + m) * ROW + 2 * kQBlk);
         #pragma unroll
         for (int q = 0; q < NT; ++q)
             #pragma unroll
-            for (int i = 0; i < 4; ++i) total[q][i] = mine ? __builtin_fmaf(share, part[0][q][i], total[q][i]) : total[q][i];
+            for (int i = 0; i < 4; ++i) total[q][i] = mine ? __builtin_fmaf(share, part[0][q][i] * down, total[q][i]) : total[q][i];
     };
     auto multiply = [&](const Turn& t) {
         const bool ahead = t.off[P] <= 4 * NX;
         if (ahead)
             #pragma unroll
-            for (int q = 0; q < NX; ++q) if (slot + 4 * q < t.off[P]) q_store8<false>(xs + (slot + 4 * q) * ROW, lane & 15, t.v[q]);
+            for (int q = 0; q < NX; ++q) {
+                const int i = slot + 4 * q;
+                const bool first = i < t.off[1];        // (before the second unit's rows: the first one's values and remainders)
+                if (i < t.off[P]) stage(t.v[q], xs + (first ? i : t.off[1] + i) * ROW, first ? t.off[1] : t.off[P] - t.off[1]);
+            }
         #pragma unroll
         for (int p = 0; p < P; ++p)
             if (t.mask[p]) {
-                if (!ahead) {                           // many tokens on few experts: a unit's rows at a time
+                if (!ahead) {                           // many tokens on few experts: a unit's at a time
                     const int ntok = __popc(t.mask[p]), col = column(t.act[p], t.kb[p]);
-                    for (int r = slot; r < 2 * ntok; r += 4) q_store8<false>(xs + r * ROW, lane & 15, values(t.act[p], r, ntok, col));
+                    for (int m = slot; m < ntok; m += 4) {
+                        f32x4 v[2];
+                        load(t.act[p], m, col, v);
+                        stage(v, xs + m * ROW, ntok);
+                    }
                 }
                 wave_lds_sync();
-                multiply_unit(t, p, ahead ? t.off[p] : 0);
+                multiply_unit(t, p, ahead ? 2 * t.off[p] : 0);
                 __builtin_amdgcn_sched_barrier(0);
                 wave_lds_sync();
             }

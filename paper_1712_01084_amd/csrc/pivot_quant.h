@@ -124,7 +124,7 @@ struct MoeLaunch {
     const int32_t* prow_down;
     const void* x; int64_t ldx; float* y; int64_t ldy; int tokens; int32_t* ids; float* weights;
     uint32_t* tickets; float* partials;                   // of the strips of the down layers
-    MoeRoute* route; float* logits; uint16_t* h;          // h: [2][tokens * top_k][F_pad] fp16, value and remainder
+    MoeRoute* route; float* logits; float* h;             // h: [tokens * top_k][F_pad]
     void* stream;
 };
 int launch_moe(const MoeLaunch& L);

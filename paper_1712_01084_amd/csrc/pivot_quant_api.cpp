@@ -127,7 +127,7 @@ MoeScratch moe_scratch(const pivot_moe_plan_t* p, int tokens) {
     s.logits = s.tickets + strips * kQTicketStride * 4;
     s.partials = s.logits + align_up((size_t)tokens * p->E * 4, 256);
     s.h = s.partials + align_up(strips * kMoeMaxParts * kQStrip * tokens * 4, 256);
-    s.x = s.h + align_up((size_t)2 * tokens * p->top_k * p->down[0]->host.K_pad * 2, 256);
+    s.x = s.h + align_up((size_t)tokens * p->top_k * p->down[0]->host.K_pad * 4, 256);
     s.total = s.x + (p->norm_weight ? align_up((size_t)tokens * align_up(p->D, 8) * 2, 256) : 0);
     return s;
 }
@@ -380,7 +380,7 @@ int pivot_moe_run(const pivot_moe_plan_t* plan, const void* x_dev, int xtype, in
     L.E = plan->E; L.top_k = plan->top_k; L.D = plan->D; L.F = plan->F; L.F_pad = hs[1]->K_pad; L.prow_down = plan->down[0]->dev.prow_pad;
     L.y = y_dev; L.ldy = ldy; L.tokens = tokens; L.ids = ids_dev; L.weights = weights_dev;
     L.tickets = reinterpret_cast<uint32_t*>(ws + s.tickets); L.partials = reinterpret_cast<float*>(ws + s.partials);
-    L.route = reinterpret_cast<MoeRoute*>(ws + s.route); L.logits = reinterpret_cast<float*>(ws + s.logits); L.h = reinterpret_cast<uint16_t*>(ws + s.h);
+    L.route = reinterpret_cast<MoeRoute*>(ws + s.route); L.logits = reinterpret_cast<float*>(ws + s.logits); L.h = reinterpret_cast<float*>(ws + s.h);
     L.stream = stream;
     return launch_moe(L);
 }
