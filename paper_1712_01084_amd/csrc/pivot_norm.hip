@@ -24,12 +24,16 @@ typedef _Float16 f16x8_any __attribute__((ext_vector_type(8), aligned(2)));
 // Eight neighbouring elements as they lie in memory, the first `n` of them real (the others 0).  Loading and converting are
 // apart, so that no load of a row waits for another.
 struct NormRaw { u32x4 a, b; };
-__device__ __forceinline__ void norm_load(const void* p, int type, long long at, int n, NormRaw& r) {
+// (the weaker alignment of a type is lost where the type is a template's argument, so this is no gload)
+__device__ __forceinline__ u32x4 norm_load16(const void* p) {
     typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+    return *(const __attribute__((address_space(1))) u32x4_any*)p;
+}
+__device__ __forceinline__ void norm_load(const void* p, int type, long long at, int n, NormRaw& r) {
     const char* q = reinterpret_cast<const char*>(p) + at * (type == PIVOT_F32 ? 4 : 2);
     if (n >= 8) {
-        r.a = gload<u32x4_any>(q);
-        if (type == PIVOT_F32) r.b = gload<u32x4_any>(q + 16);
+        r.a = norm_load16(q);
+        if (type == PIVOT_F32) r.b = norm_load16(q + 16);
         return;
     }
     #pragma unroll
