@@ -494,8 +494,8 @@ int    pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch,
  *
  *     h = x + res        res_out = h        out = weight * h / sqrt(mean(h^2) + eps)
  *
- * What stands before a layer in a network of residual blocks.  h is not rounded before it is normalised (res_out is,
- * to its type).  With otype PIVOT_Q8 a row comes out as 8-bit integers and one scale, as pivot_qfc_run takes it:
+ * What stands before a layer in a network of residual blocks.  h is normalised in fp32 where x and res are fp16, and
+ * in 64 bits where one of them is fp32 or the output is PIVOT_Q8 (res_out is rounded to its type).  With otype PIVOT_Q8 a row comes out as 8-bit integers and one scale, as pivot_qfc_run takes it:
  * scale = max |out| / 127, integer = out / scale rounded to nearest, ties to even, computed in 64 bits.  A row of
  * zeros gives scale 0 and integers 0; a row with an infinity or NaN gives scale NaN and integers 0.
  *

@@ -2,9 +2,9 @@
 //
 //     h = x + res,   out = weight * h / sqrt(mean(h^2) + eps);   8 bits: max |out| / 127 is one step
 //
-// TPR threads share a row, eight neighbouring columns each at a time, and keep weight * h in registers between the two
+// TPR threads share a row, eight neighbouring columns each at a time, and keep weight * h (or both) in registers between the two
 // passes (sum of squares and largest weight * h, then the outputs); what of a row does not fit there is read a second
-// time.  8192x4096, residual and output fp16: 54 us = 5.0 TB/s, what a copy reaches; fp32 into 8 bits 83 us = 5.2; fp16 into 8
+// time.  8192x4096, residual and output fp16: 51 us = 5.2 TB/s, what a copy reaches; fp32 into 8 bits 84 us = 5.2; fp16 into 8
 // bits 62 us = 3.8, bound by the 64-bit operations.  One row of 4096: 3.1 us, 3.6 into 8 bits, 5.4 in block order: launch, one
 // trip, two reductions, stores.  Rows of up to 16384 columns are kept whole; 64x9203 fp32 into fp16 5.3 us.
 // The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
@@ -108,12 +108,14 @@ __device__ __forceinline__ int code_of(double v, double inv) {
 
 }  // namespace
 
-// Q8: weight * h in 64 bits, else in 32.  Of the 64-bit operations (a large part of the time of 8-bit rows from fp16) a column
-// costs nine: three conversions, h, h^2 into the sum, weight * h, the maximum, and two for the code.
-template <bool Q8, bool ORDER, int TPR, int KEEP>
+// WIDE: h and weight * h in 64 bits, for 8-bit rows and where an input is fp32: its sums and products may leave the range of
+// fp32 where the output does not.  Rows of fp16 stay far inside it as long as h / rms is formed first; 64 bits would cost them
+// more than the memory hides (8192x4096 fp16 into fp16 53 -> 58 us, 100000x300 83 -> 106; fp32 into fp32 93 -> 95).
+template <bool Q8, bool WIDE, bool ORDER, int TPR, int KEEP>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch a) {
     constexpr int NT = TPR < 256 ? 256 : TPR, NW = TPR / 64;
-    typedef typename std::conditional<Q8, double, float>::type H;   // h and weight * h
+    typedef typename std::conditional<WIDE, double, float>::type H;
+    static_assert(WIDE || !Q8, "8-bit codes are computed in 64 bits");
     __shared__ double s_sum[NT / 64], s_most[NT / 64];
     extern __shared__ __align__(16) char s_row[];       // the output row, where it is put together there
     const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = q_wave();
@@ -140,9 +142,10 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
     };
     double sum = 0.0, most = 0.0;
     float bad = 0.f;                                    // NaN once anything is infinite or NaN
-    // weight * h of a piece; the sums on the first pass, what goes back to the residual on the last one
-    auto combine = [&](int c, const Piece& p, H (&hw)[8], bool first, bool last) {
-        float back[8], px[8], pr[8] = {}, pw[8];
+    // weight * h of a piece (not WIDE: h, and the weights); the sums on the first pass, what goes back to the residual on the
+    // last one
+    auto combine = [&](int c, const Piece& p, H (&hw)[8], float (&pw)[8], bool first, bool last) {
+        float back[8], px[8], pr[8] = {};
         norm_floats(p.x, a.xtype, px);
         if (a.res) norm_floats(p.r, a.rtype, pr);
         if (a.weight) norm_floats(p.w, PIVOT_F32, pw);
@@ -154,11 +157,11 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
             const float x = px[i], r = pr[i], w = pw[i];
             const H h = (H)x + (H)r;
             back[i] = x + r;
-            hw[i] = h * (H)w;
+            hw[i] = WIDE ? h * (H)w : h;
             if (first) {
                 sum = __builtin_fma((double)h, (double)h, sum);
-                if (Q8) {
-                    most = __builtin_fmax(most, __builtin_fabs((double)hw[i]));
+                if constexpr (Q8) {
+                    most = __builtin_fmax(most, __builtin_fabs(hw[i]));
                     bad = __builtin_fmaf(x, 0.f, __builtin_fmaf(r, 0.f, __builtin_fmaf(w, 0.f, bad)));
                 }
             }
@@ -166,18 +169,20 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         if (last && a.res_out) norm_store(a.res_out, a.rtype, so + c, a.cols - c, back);
     };
     H keep[KEEP][8];
+    float kept_w[KEEP][8];
     {
         Piece p[KEEP];
         #pragma unroll
         for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) fetch((tid + k * TPR) * 8, p[k]);
         #pragma unroll
-        for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) combine((tid + k * TPR) * 8, p[k], keep[k], true, true);
+        for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) combine((tid + k * TPR) * 8, p[k], keep[k], kept_w[k], true, true);
     }
     for (int c = (tid + KEEP * TPR) * 8; c < a.cols; c += TPR * 8) {
         Piece p;
         H hw[8];
+        float pw[8];
         fetch(c, p);
-        combine(c, p, hw, true, false);
+        combine(c, p, hw, pw, true, false);
     }
     if (Q8 && bad != bad) most = __builtin_inf();
     sum = wave64(sum, [](double u, double v) { return u + v; });
@@ -197,11 +202,11 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
     }
     const bool fine = most > 0.0 && most < __builtin_inf();
     const double inv = Q8 && fine ? 127.0 / most : 0.0;
-    float rs = 0.f;
-    if (!Q8) rs = (float)(1.0 / sqrt(sum / a.cols + (double)a.eps));
+    H rs = 0;
+    if (!Q8) rs = (H)(1.0 / sqrt(sum / a.cols + (double)a.eps));
     else if (tid == 0)                                   // the only use of it: the codes do not depend on the sum
         a.scale[row] = fine ? (float)(most / sqrt(sum / a.cols + (double)a.eps) / 127.0) : (most == 0.0 ? 0.f : __builtin_nanf(""));
-    auto finish = [&](int c, const H (&hw)[8], const int* at) {
+    auto finish = [&](int c, const H (&hw)[8], const float (&pw)[8], const int* at) {
         const int n = a.cols - c;
         if constexpr (Q8) {
             int code[8];
@@ -224,7 +229,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         } else {
             float v[8];
             #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = hw[i] * rs;
+            for (int i = 0; i < 8; ++i) v[i] = WIDE ? (float)(hw[i] * rs) : (float)(hw[i] * rs) * pw[i];
             if (!ORDER) norm_store(a.out, a.otype, oo + c, n, v);
             else {
                 char* to = a.lds_rows ? mine : reinterpret_cast<char*>(a.out) + oo * es;
@@ -239,13 +244,14 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
         }
     };
     #pragma unroll
-    for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) finish((tid + k * TPR) * 8, keep[k], ORDER ? place[k] : nullptr);
+    for (int k = 0; k < KEEP; ++k) if ((tid + k * TPR) * 8 < a.cols) finish((tid + k * TPR) * 8, keep[k], kept_w[k], ORDER ? place[k] : nullptr);
     for (int c = (tid + KEEP * TPR) * 8; c < a.cols; c += TPR * 8) {
         Piece p;
         H hw[8];
+        float pw[8];
         fetch(c, p);
-        combine(c, p, hw, false, true);
-        finish(c, hw, nullptr);
+        combine(c, p, hw, pw, false, true);
+        finish(c, hw, pw, nullptr);
     }
     if (ORDER && a.lds_rows) {
         if (NW > 1) __syncthreads(); else wave_lds_sync();
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
 
 namespace {
 
-template <bool Q8, bool ORDER>
+template <bool Q8, bool WIDE, bool ORDER>
 int norm_go(NormLaunch a) {
     hipStream_t st = reinterpret_cast<hipStream_t>(a.stream);
     auto go = [&](auto k, int per, int threads) {
@@ -273,17 +279,18 @@ int norm_go(NormLaunch a) {
         return PIVOT_OK;
     };
     const bool many = a.rows >= 512;                      // rows enough to fill the device with few threads each
-    if (a.cols <= 64 * 8 && (many || a.cols <= 64)) return go(norm_kernel<Q8, ORDER, 64, 1>, 4, 256);
-    if (a.cols <= 256 * 8) return go(norm_kernel<Q8, ORDER, 256, 1>, 1, 256);
-    if (a.cols <= 512 * 8 && many) return go(norm_kernel<Q8, ORDER, 512, 1>, 1, 512);
-    return a.cols <= 1024 * 8 ? go(norm_kernel<Q8, ORDER, 1024, 1>, 1, 1024) : go(norm_kernel<Q8, ORDER, 1024, 2>, 1, 1024);
+    if (a.cols <= 64 * 8 && (many || a.cols <= 64)) return go(norm_kernel<Q8, WIDE, ORDER, 64, 1>, 4, 256);
+    if (a.cols <= 256 * 8) return go(norm_kernel<Q8, WIDE, ORDER, 256, 1>, 1, 256);
+    if (a.cols <= 512 * 8 && many) return go(norm_kernel<Q8, WIDE, ORDER, 512, 1>, 1, 512);
+    return a.cols <= 1024 * 8 ? go(norm_kernel<Q8, WIDE, ORDER, 1024, 1>, 1, 1024) : go(norm_kernel<Q8, WIDE, ORDER, 1024, 2>, 1, 1024);
 }
 
 }  // namespace
 
 int launch_norm(const NormLaunch& a) {
-    if (a.otype == PIVOT_Q8) return a.order ? norm_go<true, true>(a) : norm_go<true, false>(a);
-    return a.order ? norm_go<false, true>(a) : norm_go<false, false>(a);
+    if (a.otype == PIVOT_Q8) return a.order ? norm_go<true, true, true>(a) : norm_go<true, true, false>(a);
+    if (a.xtype == PIVOT_F32 || (a.res && a.rtype == PIVOT_F32)) return a.order ? norm_go<false, true, true>(a) : norm_go<false, true, false>(a);
+    return a.order ? norm_go<false, false, true>(a) : norm_go<false, false, false>(a);
 }
 
 }  // namespace pivot
