@@ -24,6 +24,7 @@ PIVOT_W_NATURAL, PIVOT_W_PIVOTED = 0, 1
 PIVOT_MLP_KEEP_FINAL_BLOCK_ORDER = 1
 PIVOT_MLP_LAUNCH_PER_LAYER = 2
 PIVOT_QFC_X_BLOCK_ORDER = 1
+PIVOT_QFC_WEIGHTS_ON_DEVICE = 1
 PIVOT_MOE_RENORMALISE = 1
 
 PIVOT_OK = 0
@@ -402,19 +403,21 @@ def _array(a, dtype, shape, name):
 
 def pivot_qfc_plan(M, K, bh, bw, group, codes, scales, zeros=None, tile_mask=None, prow=None, pcol=None, bias=None, *,
                    act=PIVOT_ACT_NONE, chunk_blocks=0, device=-1, flags=0):
-    """Host numpy arrays in (codes: [M][ceil(K/2)] bytes, scales: [M][ceil(K/group)] fp16), opaque plan handle out."""
+    """Host numpy arrays in (codes: [M][ceil(K/2)] bytes, scales: [M][ceil(K/group)] fp16), opaque plan handle out.  With
+    PIVOT_QFC_WEIGHTS_ON_DEVICE among the flags codes, scales, zeros and bias are device addresses of such arrays."""
     d = pivot_qfc_desc(M, K, bh, bw, group, act, chunk_blocks, device, flags)
     if min(M, K, bh, bw, group) > 0:      # the library refuses the rest
         ng = -(-K // group)
-        codes = _array(codes, np.uint8, (M, -(-K // 2)), "codes")
-        scales = _array(scales, np.float16, (M, ng), "scales")
-        zeros = _array(zeros, np.uint8, (M, ng), "zeros")
+        if not flags & PIVOT_QFC_WEIGHTS_ON_DEVICE:
+            codes = _array(codes, np.uint8, (M, -(-K // 2)), "codes")
+            scales = _array(scales, np.float16, (M, ng), "scales")
+            zeros = _array(zeros, np.uint8, (M, ng), "zeros")
+            bias = _array(bias, np.float32, (M,), "bias")
         tile_mask = _array(tile_mask, np.uint8, (-(-M // bh), -(-K // bw)), "tile_mask")
         prow, pcol = _array(prow, np.int32, (M,), "prow"), _array(pcol, np.int32, (K,), "pcol")
-        bias = _array(bias, np.float32, (M,), "bias")
     out = C.c_void_p()
-    _check(lib().pivot_qfc_plan(C.byref(d), _np_ptr(codes), _np_ptr(scales), _np_ptr(zeros), _np_ptr(tile_mask), _np_ptr(prow),
-                                _np_ptr(pcol), _np_ptr(bias), C.byref(out)))
+    weights = [w if isinstance(w, int) else _np_ptr(w) for w in (codes, scales, zeros, bias)]
+    _check(lib().pivot_qfc_plan(C.byref(d), *weights[:3], _np_ptr(tile_mask), _np_ptr(prow), _np_ptr(pcol), weights[3], C.byref(out)))
     return out
 
 
@@ -465,7 +468,9 @@ def pivot_moe_plan(gate_up, down, top_k, router, *, router_bias=None, norm_weigh
     if router.dtype not in (np.float32, np.float16):
         raise PivotError(PIVOT_E_UNSUPPORTED, "the router's matrix must be fp32 or fp16")
     if n:
-        D = pivot_qfc_plan_host_view(gate_up[0])["K"]
+        view = pivot_qfc_view()
+        _check(lib().pivot_qfc_plan_host_view(gate_up[0], C.byref(view)))
+        D = view.K
         router = _array(router, router.dtype, (n, D), "router")
         router_bias = _array(router_bias, np.float32, (n,), "router_bias")
         norm_weight = _array(norm_weight, np.float32, (D,), "norm_weight")

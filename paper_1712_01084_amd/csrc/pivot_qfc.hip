@@ -1,10 +1,18 @@
 // Layers with 4-bit weights: laying the weights out on the device, and the choice of a launch.
+#include <algorithm>
 #include <mutex>
 #include <unordered_map>
 
 #include "pivot_qfc_kernel.h"
 
 namespace pivot {
+
+// What laying out needs.
+struct QfcPack {
+    u32x4* codes; uint16_t* scales; uint8_t* zeros; const uint8_t* raw_codes; const uint16_t* raw_scales; const uint8_t* raw_zeros;
+    const int32_t* row_of_kb; const int32_t* kb_ptr; const int32_t* pieces; int32_t* bad;
+    int M, K, bh, bw, group, gpk;
+};
 
 int reserve_lds(const void* kernel, size_t bytes) {
     constexpr int kMost = 144 * 1024;                            // leaves 16 KB of a compute unit for what kernels declare
@@ -31,45 +39,69 @@ int reserve_lds(const void* kernel, size_t bytes) {
     return PIVOT_E_HIP;
 }
 
-// One wavefront per unit: lane l gathers the 32 codes of row l % 16 that it will multiply, and the unit's scales.
-__global__ void __launch_bounds__(64) qfc_pack_kernel(u32x4* codes, uint16_t* scales, uint8_t* zeros, const uint8_t* raw_codes,
-                                                      const uint16_t* raw_scales, const uint8_t* raw_zeros, const int32_t* row_of_kb,
-                                                      const int32_t* kb_ptr, const int32_t* pieces, int M, int K, int bh, int bw, int group, int gpk) {
-    const int lane = threadIdx.x, kb = blockIdx.x, s = blockIdx.y;
-    const int br = row_of_kb[kb], first = kb_ptr[br], nkb = kb_ptr[br + 1] - first, ppb = kQBlk / bw;
-    const size_t unit = (size_t)first * (bh / kQStrip) + (size_t)s * nkb + (kb - first);
-    const int row = br * bh + s * kQStrip + (lane & 15);
-    const long long code_ld = (K + 1) / 2, group_ld = (K + group - 1) / group;
+// One wavefront per unit: lane l gathers the 32 codes of row l % 16 that it will multiply, eight neighbouring columns of the
+// caller's rows at a time, and the unit's scales.  bad: set where a zero point is above 15.
+__global__ void __launch_bounds__(256) qfc_pack_kernel(QfcPack p, int kb0, int kb1) {
+    const int lane = threadIdx.x & 63, kb = kb0 + blockIdx.x * 4 + q_wave(), s = blockIdx.y;
+    if (kb >= kb1) return;
+    const int br = p.row_of_kb[kb], first = p.kb_ptr[br], nkb = p.kb_ptr[br + 1] - first, ppb = kQBlk / p.bw, row0 = br * p.bh + s * kQStrip;
+    const size_t unit = (size_t)first * (p.bh / kQStrip) + (size_t)s * nkb + (kb - first);
+    const int row = row0 + (lane & 15);
+    const long long code_ld = (p.K + 1) / 2, group_ld = (p.K + p.group - 1) / p.group;
     uint32_t w[4];
+    #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        w[j] = 0;
-        for (int i = 0; i < 8; ++i) {
-            const int c = 32 * j + 8 * (lane >> 4) + q_nibble_col(i);
-            const int p = pieces[kb * ppb + c / bw], col = p + c % bw;
-            uint32_t q = 8;                                     // padding: a weight of zero
-            if (p >= 0 && row < M && col < K) q = (raw_codes[row * code_ld + col / 2] >> (4 * (col & 1))) & 15u;
-            w[j] |= q << (4 * i);
+        const int c = 32 * j + 8 * (lane >> 4), piece = p.pieces[(size_t)kb * ppb + c / p.bw], col = piece + c % p.bw;
+        uint32_t v = 0x88888888u;                               // padding: weights of zero
+        if (piece >= 0 && row < p.M && col < p.K) {
+            const uint8_t* q = p.raw_codes + row * code_ld + col / 2;
+            if (col + 8 <= p.K) {
+                typedef uint32_t word_any __attribute__((aligned(1)));
+                v = *reinterpret_cast<const word_any*>(q);
+            } else
+                for (int i = 0; i < p.K - col; ++i) v = (v & ~(15u << (4 * i))) | (uint32_t)((q[i / 2] >> (4 * (i & 1))) & 15) << (4 * i);
+        }
+        // nibble i holds column q_nibble_col(i): the even columns, then the odd ones
+        const auto gather = [](uint32_t n) { n &= 0x0f0f0f0fu; n = (n | n >> 4) & 0x00ff00ffu; return (n | n >> 8) & 0xffffu; };
+        w[j] = gather(v) | gather(v >> 4) << 16;
+    }
+    p.codes[unit * 64 + lane] = u32x4{w[0], w[1], w[2], w[3]};
+    for (int e = lane; e < p.gpk * kQStrip; e += 64) {
+        const int g = e / kQStrip, i = e % kQStrip, r = row0 + i, c = g * (kQBlk / p.gpk);
+        const int piece = p.pieces[(size_t)kb * ppb + c / p.bw], col = piece + c % p.bw;
+        const bool real = piece >= 0 && r < p.M && col < p.K;
+        const long long at = r * group_ld + col / p.group;
+        p.scales[((unit * 4 + i / 4) * p.gpk + g) * 4 + i % 4] = real ? p.raw_scales[at] : (uint16_t)0;
+        if (p.zeros) {
+            const uint8_t z = real ? p.raw_zeros[at] : (uint8_t)8;
+            p.zeros[(unit * kQStrip + i) * p.gpk + g] = z;
+            if (z > 15) *p.bad = 1;
         }
     }
-    codes[unit * 64 + lane] = u32x4{w[0], w[1], w[2], w[3]};
-    for (int e = lane; e < gpk * kQStrip; e += 64) {
-        const int g = e / kQStrip, r = br * bh + s * kQStrip + e % kQStrip, c = g * (kQBlk / gpk);
-        const int p = pieces[kb * ppb + c / bw], col = p + c % bw;
-        const bool real = p >= 0 && r < M && col < K;
-        const int i = e % kQStrip;
-        scales[((unit * 4 + i / 4) * gpk + g) * 4 + i % 4] = real ? raw_scales[r * group_ld + col / group] : (uint16_t)0;
-        if (zeros) zeros[(unit * kQStrip + i) * gpk + g] = real ? raw_zeros[r * group_ld + col / group] : (uint8_t)8;
-    }
+}
+static_assert(q_nibble_col(1) == 2 && q_nibble_col(3) == 6 && q_nibble_col(4) == 1 && q_nibble_col(7) == 7, "the order of the nibbles");
+
+// The bias in block order.
+__global__ void __launch_bounds__(256) qfc_bias_kernel(float* bias_p, const float* bias, const int32_t* prow, int M_pad) {
+    const int r = blockIdx.x * 256 + threadIdx.x;
+    if (r < M_pad) bias_p[r] = prow[r] >= 0 ? bias[prow[r]] : 0.f;
 }
 
 int launch_qfc_pack(const QfcHost& h, const QfcDev& d, const uint8_t* raw_codes, const uint16_t* raw_scales, const uint8_t* raw_zeros,
-                    const int32_t* row_of_kb) {
-    if (h.KB == 0) return PIVOT_OK;
-    hipLaunchKernelGGL(qfc_pack_kernel, dim3(h.KB, h.strips()), dim3(64), 0, nullptr, reinterpret_cast<u32x4*>(d.codes), d.scales, d.zeros, raw_codes, raw_scales, raw_zeros,
-                       row_of_kb, d.kb_ptr, d.pieces, h.d.M, h.d.K, h.d.bh, h.d.bw, h.d.group, h.gpk);
+                    const float* raw_bias) {
+    const QfcPack p{reinterpret_cast<u32x4*>(d.codes), d.scales, d.zeros, raw_codes, raw_scales, raw_zeros, d.row_of_kb, d.kb_ptr, d.pieces,
+                    d.bad, h.d.M, h.d.K, h.d.bh, h.d.bw, h.d.group, h.gpk};
+    constexpr int kSlice = 1 << 24;                             // (a launch has less than 2^32 threads)
+    for (int kb = 0; kb < h.KB; kb += kSlice) {
+        const int end = std::min(h.KB, kb + kSlice);
+        hipLaunchKernelGGL(qfc_pack_kernel, dim3((end - kb + 3) / 4, h.strips()), dim3(256), 0, nullptr, p, kb, end);
+    }
+    if (raw_bias) hipLaunchKernelGGL(qfc_bias_kernel, dim3((h.M_pad + 255) / 256), dim3(256), 0, nullptr, d.bias_p, raw_bias, d.prow_pad, h.M_pad);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
-    if (e != hipSuccess) { set_error("laying out the weights failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
+    int32_t zero_above_15 = 0;
+    if (e == hipSuccess) e = raw_zeros ? hipMemcpy(&zero_above_15, d.bad, sizeof(int32_t), hipMemcpyDeviceToHost) : hipStreamSynchronize(nullptr);
+    if (e != hipSuccess) { (void)hipGetLastError(); set_error("laying out the weights failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
+    if (zero_above_15) { set_error("a zero point is above 15"); return PIVOT_E_SHAPE; }
     return PIVOT_OK;
 }
 

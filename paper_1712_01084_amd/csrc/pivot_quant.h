@@ -59,13 +59,16 @@ struct QfcDev {
     int32_t* pcol_pad = nullptr;        // [K_pad]
     int32_t* invpcol = nullptr;         // [K]
     float*   bias_p = nullptr;
+    int32_t* row_of_kb = nullptr;       // [KB] the block row of a block (laying out)
+    int32_t* bad = nullptr;             // (laying out) whether a zero point is above 15
 };
 
 int  build_qfc_host(const pivot_qfc_desc& d, const uint8_t* zeros, int64_t groups, const uint8_t* tile_mask, const int32_t* prow,
                     const int32_t* pcol, const float* bias, QfcHost& h);
-// Lays the codes and scales out on the device; raw_*: the caller's arrays, already there.
+// Lays the codes and scales out on the device, and waits for it; raw_*: the caller's arrays, there already (raw_bias NULL:
+// bias_p stands).
 int  launch_qfc_pack(const QfcHost& h, const QfcDev& d, const uint8_t* raw_codes, const uint16_t* raw_scales,
-                     const uint8_t* raw_zeros, const int32_t* row_of_kb);
+                     const uint8_t* raw_zeros, const float* raw_bias);
 
 struct QfcLaunch {
     const QfcHost* h; const QfcDev* d;

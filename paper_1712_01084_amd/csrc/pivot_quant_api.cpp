@@ -49,16 +49,27 @@ int put(void* dst, const void* src, size_t bytes) {
     return e == hipSuccess ? PIVOT_OK : hip_error("hipMemcpy to device", e);
 }
 
-// Weights and index arrays of a plan in one allocation; the caller's codes and scales pass through a second one that is
-// freed again.
-int upload(pivot_qfc_plan_t* p, const uint8_t* codes, const void* scales, const uint8_t* zeros) {
+// Whether `p` is memory of this device.
+bool on_device(const void* p, int device) {
+    hipPointerAttribute_t at{};
+    if (hipPointerGetAttributes(&at, p) != hipSuccess) { (void)hipGetLastError(); return false; }
+    return at.type == hipMemoryTypeDevice && at.device == device;
+}
+
+// Weights and index arrays of a plan in one allocation, the index arrays in one copy.  Weights in host memory pass through a
+// second allocation that is freed again.
+int upload(pivot_qfc_plan_t* p, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, const float* bias) {
     const QfcHost& h = p->host;
     QfcDev& d = p->dev;
+    const bool there = h.d.flags & PIVOT_QFC_WEIGHTS_ON_DEVICE;
     DeviceGuard g(p->device);
     if (!g.ok) { set_error("cannot select device %d", p->device); return PIVOT_E_HIP; }
+    if (there)
+        for (const void* q : {(const void*)codes, (const void*)scales, (const void*)zeros, (const void*)bias})
+            if (q && !on_device(q, p->device)) { set_error("PIVOT_QFC_WEIGHTS_ON_DEVICE: codes, scales, zeros and bias must be memory of device %d", p->device); return PIVOT_E_UNSUPPORTED; }
     std::vector<int32_t> row_of_kb(h.KB);
-    for (int i = 0; i < h.nbr; ++i)
-        for (int k = h.kb_ptr[i]; k < h.kb_ptr[i + 1]; ++k) row_of_kb[k] = i;
+    for (int i = 0; i < h.nbr; ++i) std::fill(row_of_kb.begin() + h.kb_ptr[i], row_of_kb.begin() + h.kb_ptr[i + 1], i);
+    const int32_t none = 0;
     const size_t units = h.units(), ns = units * h.gpk * kQStrip;
     struct Piece { const void* src; size_t bytes; void** dst; };
     const Piece pieces[] = {
@@ -72,32 +83,42 @@ int upload(pivot_qfc_plan_t* p, const uint8_t* codes, const void* scales, const 
         {h.pcol_pad.data(), h.pcol_pad.size() * 4, (void**)&d.pcol_pad},
         {h.invpcol.data(), h.invpcol.size() * 4, (void**)&d.invpcol},
         {h.bias_p.data(), h.bias_p.size() * 4, (void**)&d.bias_p},
+        {row_of_kb.data(), row_of_kb.size() * 4, (void**)&d.row_of_kb},
+        {&none, sizeof(none), (void**)&d.bad},
     };
-    size_t total = 0;
-    for (const Piece& q : pieces) total += align_up(q.bytes + 1, 256);
+    constexpr int kLaidOut = 3;                         // the pieces that are made there; behind them those that are copied
+    size_t total = 0, copied_from = 0;
+    for (const Piece& q : pieces) {
+        if (&q == pieces + kLaidOut) copied_from = total;
+        total += align_up(q.bytes + 1, 256);
+    }
     DeviceMemory mem, raw;
     int rc = mem.get(total);
     if (rc != PIVOT_OK) return rc;
+    std::vector<char> image(total - copied_from);
     size_t off = 0;
     for (const Piece& q : pieces) {
         *q.dst = mem.p + off;
-        if (q.src && (rc = put(mem.p + off, q.src, q.bytes)) != PIVOT_OK) { d = QfcDev{}; return rc; }
+        if (off >= copied_from && q.bytes) memcpy(image.data() + (off - copied_from), q.src, q.bytes);
         off += align_up(q.bytes + 1, 256);
     }
     if (!h.has_zeros) d.zeros = nullptr;
-    const size_t code_bytes = (size_t)h.d.M * ((h.d.K + 1) / 2), ngroups = (size_t)h.d.M * ((h.d.K + h.d.group - 1) / h.d.group);
-    const size_t o1 = align_up(code_bytes, 256), o2 = o1 + align_up(ngroups * 2, 256), o3 = o2 + (zeros ? align_up(ngroups, 256) : 0);
-    if (h.KB > 0) {
-        rc = raw.get(o3 + (size_t)h.KB * 4);
-        if (rc == PIVOT_OK) rc = put(raw.p, codes, code_bytes);
-        if (rc == PIVOT_OK) rc = put(raw.p + o1, scales, ngroups * 2);
-        if (rc == PIVOT_OK && zeros) rc = put(raw.p + o2, zeros, ngroups);
-        if (rc == PIVOT_OK) rc = put(raw.p + o3, row_of_kb.data(), (size_t)h.KB * 4);
-        if (rc == PIVOT_OK)
-            rc = launch_qfc_pack(h, d, reinterpret_cast<const uint8_t*>(raw.p), reinterpret_cast<const uint16_t*>(raw.p + o1),
-                                 zeros ? reinterpret_cast<const uint8_t*>(raw.p + o2) : nullptr, reinterpret_cast<const int32_t*>(raw.p + o3));
-        if (rc != PIVOT_OK) { d = QfcDev{}; return rc; }
+    rc = put(mem.p + copied_from, image.data(), image.size());
+    if (rc == PIVOT_OK && !there) {
+        const size_t code_bytes = (size_t)h.d.M * ((h.d.K + 1) / 2), ngroups = (size_t)h.d.M * ((h.d.K + h.d.group - 1) / h.d.group);
+        const size_t o1 = align_up(code_bytes, 256), o2 = o1 + align_up(ngroups * 2, 256);
+        if (h.KB > 0) {
+            rc = raw.get(o2 + ngroups);
+            if (rc == PIVOT_OK) rc = put(raw.p, codes, code_bytes);
+            if (rc == PIVOT_OK) rc = put(raw.p + o1, scales, ngroups * 2);
+            if (rc == PIVOT_OK && zeros) rc = put(raw.p + o2, zeros, ngroups);
+            codes = reinterpret_cast<const uint8_t*>(raw.p);
+            scales = reinterpret_cast<const uint16_t*>(raw.p + o1);
+            zeros = reinterpret_cast<const uint8_t*>(raw.p + o2);
+        }
     }
+    if (rc == PIVOT_OK) rc = launch_qfc_pack(h, d, codes, scales, zeros, there ? bias : nullptr);
+    if (rc != PIVOT_OK) { d = QfcDev{}; return rc; }
     d.base = mem.release();
     return PIVOT_OK;
 }
@@ -145,10 +166,15 @@ int pivot_qfc_plan(const pivot_qfc_desc* desc, const uint8_t* codes, const void*
     if (!p) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
     // (sizes that the builder refuses are not looked through)
     const int64_t groups = desc->M > 0 && desc->K > 0 && desc->group > 0 ? (int64_t)desc->M * (((int64_t)desc->K + desc->group - 1) / desc->group) : 0;
-    int rc = build_qfc_host(*desc, zeros, groups, tile_mask, prow, pcol, bias, p->host);
+    const bool there = desc->flags & PIVOT_QFC_WEIGHTS_ON_DEVICE;      // (what lies there is not read here)
+    int rc = PIVOT_OK;
+    if (there && desc->device < 0) { set_error("PIVOT_QFC_WEIGHTS_ON_DEVICE needs a device"); rc = PIVOT_E_NO_DEVICE; }
+    if (there && (!aligned_to(scales, 2) || !aligned_to(bias, 4))) { set_error("scales and bias must be aligned to their type"); rc = PIVOT_E_SHAPE; }
+    if (rc == PIVOT_OK) rc = build_qfc_host(*desc, there ? nullptr : zeros, groups, tile_mask, prow, pcol, there ? nullptr : bias, p->host);
+    if (there) p->host.has_zeros = zeros != nullptr;
     if (rc == PIVOT_OK && desc->device >= 0) {
         p->device = desc->device;
-        try { rc = upload(p, codes, scales, zeros); }
+        try { rc = upload(p, codes, static_cast<const uint16_t*>(scales), zeros, bias); }
         catch (const std::bad_alloc&) { set_error("out of host memory"); rc = PIVOT_E_ALLOC; }
     }
     if (rc != PIVOT_OK) { delete p; return rc; }

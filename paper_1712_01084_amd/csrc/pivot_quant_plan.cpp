@@ -41,7 +41,7 @@ int build_qfc_host(const pivot_qfc_desc& d, const uint8_t* zeros, int64_t groups
     if (d.bw != 32 && d.bw != 64 && d.bw != 128) return unsupported("tile columns of a 4-bit layer must be 32, 64 or 128");
     if (d.group != 32 && d.group != 64 && d.group != 128) return unsupported("the group of a 4-bit layer must be 32, 64 or 128 columns");
     if (d.act != PIVOT_ACT_NONE && d.act != PIVOT_ACT_RELU) return unsupported("unknown activation");
-    if (d.flags != 0) return unsupported("unknown flags");
+    if (d.flags & ~PIVOT_QFC_WEIGHTS_ON_DEVICE) return unsupported("unknown flags");
     if (d.chunk_blocks < 0) { set_error("chunk_blocks must not be negative"); return PIVOT_E_SHAPE; }
     if (zeros)
         for (int64_t i = 0; i < groups; ++i)
