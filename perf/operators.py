@@ -157,9 +157,9 @@ class _State:
 
     def plan(self, L):
         from paper_1712_01084_amd import binding as B
-        host = lambda t: None if t is None else t.cpu().numpy()  # noqa: E731
-        p = B.pivot_qfc_plan(L["M"], L["K"], L["bh"], L["bw"], L["group"], host(L["codes"]), host(L["scales"]), host(L["zeros"]),
-                             L["mask"], L["prow"], L["pcol"], host(L["bias"]), act=L["act"], device=0)
+        codes, scales, zeros, bias = (None if L[k] is None else L[k].data_ptr() for k in ("codes", "scales", "zeros", "bias"))
+        p = B.pivot_qfc_plan(L["M"], L["K"], L["bh"], L["bw"], L["group"], codes, scales, zeros, L["mask"], L["prow"], L["pcol"], bias,
+                             act=L["act"], device=0, flags=B.PIVOT_QFC_WEIGHTS_ON_DEVICE)
         self.free.append((B.pivot_qfc_plan_destroy, p))
         return p
 
