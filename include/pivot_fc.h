@@ -495,7 +495,11 @@ size_t pivot_qfc_workspace_bytes(const pivot_qfc_plan_t* plan, int batch);
 #define PIVOT_QFC_X_BLOCK_ORDER 1
 int    pivot_qfc_run(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, int64_t ldx, const float* xscale_dev,
                      float* y_dev, int64_t ldy, int batch, int flags, void* ws_dev, size_t ws_bytes, void* stream);
-/* Name of the kernel instantiation pivot_qfc_run launches for this type of x and batch.  Needs no device. */
+/* Name of the instantiation of the product kernel that pivot_qfc_run launches with these arguments (a copy of x may be
+ * launched before it); x_dev is not read, NULL stands for an aligned address.  Needs no device. */
+int    pivot_qfc_run_kernel_name(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, int64_t ldx, int batch, int flags,
+                                 char* buf, size_t buf_len);
+/* ... for x in natural coordinates whose rows all begin at multiples of 16 bytes. */
 int    pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch, char* buf, size_t buf_len);
 
 /*

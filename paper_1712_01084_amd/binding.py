@@ -39,7 +39,7 @@ EXPORTS = [
     "pivot_mlp_workspace_bytes", "pivot_mlp_run", "pivot_mlp_kernel_name", "pivot_mlp_status", "pivot_mlp_status_word",
     "pivot_lstm_workspace_bytes", "pivot_lstm_run", "pivot_lstm_status", "pivot_lstm_status_word", "pivot_lstm_restore", "pivot_lstm_kernel_name",
     "pivot_dense_run", "pivot_csr_run", "pivot_null_run", "pivot_stream_read_run", "pivot_exchange_probe_run", "pivot_feedback_search",
-    "pivot_qfc_plan", "pivot_qfc_plan_host_view", "pivot_qfc_plan_destroy", "pivot_qfc_workspace_bytes", "pivot_qfc_run", "pivot_qfc_kernel_name",
+    "pivot_qfc_plan", "pivot_qfc_plan_host_view", "pivot_qfc_plan_destroy", "pivot_qfc_workspace_bytes", "pivot_qfc_run", "pivot_qfc_run_kernel_name", "pivot_qfc_kernel_name",
     "pivot_norm_run", "pivot_moe_plan", "pivot_moe_plan_destroy", "pivot_moe_workspace_bytes", "pivot_moe_run",
 ]
 
@@ -159,6 +159,7 @@ def lib():
     L.pivot_qfc_workspace_bytes.argtypes = [vp, i32]
     L.pivot_qfc_workspace_bytes.restype = sz
     L.pivot_qfc_run.argtypes = [vp, vp, i32, i64, vp, vp, i64, i32, i32, vp, sz, vp]
+    L.pivot_qfc_run_kernel_name.argtypes = [vp, vp, i32, i64, i32, i32, C.c_char_p, sz]
     L.pivot_qfc_kernel_name.argtypes = [vp, i32, i32, C.c_char_p, sz]
     L.pivot_norm_run.argtypes = [C.POINTER(pivot_norm_args), vp]
     L.pivot_moe_plan.argtypes = [C.POINTER(pivot_moe_desc), C.POINTER(vp), C.POINTER(vp), vp, vp, vp, C.POINTER(vp)]
@@ -445,8 +446,15 @@ def pivot_qfc_run(plan, x_ptr, xtype, ldx, xscale_ptr, y_ptr, ldy, batch, ws_ptr
     _check(lib().pivot_qfc_run(plan, x_ptr, xtype, ldx, xscale_ptr, y_ptr, ldy, batch, flags, ws_ptr, ws_bytes, stream))
 
 
+def pivot_qfc_run_kernel_name(plan, x_ptr, xtype, ldx, batch, *, flags=0):
+    """Name of the instantiation of the product kernel that pivot_qfc_run launches with these arguments."""
+    buf = C.create_string_buffer(256)
+    _check(lib().pivot_qfc_run_kernel_name(plan, x_ptr, xtype, ldx, batch, flags, buf, 256))
+    return buf.value.decode()
+
+
 def pivot_qfc_kernel_name(plan, xtype, batch):
-    """Name of the kernel instantiation pivot_qfc_run launches for this plan, type of x and batch."""
+    """... for x in natural coordinates whose rows all begin at multiples of 16 bytes."""
     buf = C.create_string_buffer(256)
     _check(lib().pivot_qfc_kernel_name(plan, xtype, batch, buf, 256))
     return buf.value.decode()

@@ -232,13 +232,16 @@ int pivot_qfc_run(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, in
     return launch_qfc(L);
 }
 
-int pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch, char* buf, size_t buf_len) try {
+int pivot_qfc_run_kernel_name(const pivot_qfc_plan_t* plan, const void* x_dev, int xtype, int64_t ldx, int batch, int flags, char* buf,
+                              size_t buf_len) try {
     if (!plan || !buf) { set_error("plan and buf are required"); return PIVOT_E_NULL; }
     if (buf_len == 0) { set_error("buf_len is 0"); return PIVOT_E_SHAPE; }
     if (batch < 1 || batch > 64) { set_error("batch %d outside 1..64", batch); return PIVOT_E_SHAPE; }
     if (xtype != PIVOT_F16 && xtype != PIVOT_Q8) { set_error("x of a 4-bit layer is PIVOT_F16 or PIVOT_Q8"); return PIVOT_E_UNSUPPORTED; }
+    if (flags & ~PIVOT_QFC_X_BLOCK_ORDER) { set_error("unknown flags"); return PIVOT_E_UNSUPPORTED; }
+    if (ldx < plan->host.d.K) { set_error("ldx smaller than K"); return PIVOT_E_SHAPE; }
     QfcLaunch L{};
-    L.h = &plan->host; L.d = &plan->dev; L.xtype = xtype; L.batch = batch;
+    L.h = &plan->host; L.d = &plan->dev; L.x = x_dev; L.xtype = xtype; L.ldx = ldx; L.block_order = flags & PIVOT_QFC_X_BLOCK_ORDER; L.batch = batch;
     std::string name;
     int rc = launch_qfc(L, &name);
     if (rc != PIVOT_OK) return rc;
@@ -247,6 +250,10 @@ int pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch, ch
     buf[n] = 0;
     return PIVOT_OK;
 } catch (...) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
+
+int pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch, char* buf, size_t buf_len) {
+    return pivot_qfc_run_kernel_name(plan, nullptr, xtype, plan ? (int64_t)align_up(plan->host.d.K, 16) : 0, batch, 0, buf, buf_len);
+}
 
 int pivot_norm_run(const pivot_norm_args* args, void* stream) {
     if (!args) { set_error("args is NULL"); return PIVOT_E_NULL; }
