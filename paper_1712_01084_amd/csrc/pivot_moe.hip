@@ -539,7 +539,7 @@ template <int GPK, bool ZP>
 int down_go(const MoeLaunch& L, int) {
     auto go = [&](auto k, int w, int rows) {
         // Workgroups of a strip: until there is one for every compute unit, with at least two units to a wavefront.
-        const int units = L.mean_kb[1] * std::min(L.E, L.tokens * L.top_k);
+        const int units = L.down_blocks * std::min(L.E, L.tokens * L.top_k);
         int parts = 1;
         while (parts < kMoeMaxParts && L.nstrips[1] * parts < 256 && units >= 4 * w * parts) parts *= 2;
         const size_t smem = (size_t)w * rows * QElem<false>::kRow;      // more than the sums'

@@ -96,6 +96,8 @@ int reserve_lds(const void* kernel, size_t bytes);
 constexpr int kMoeMaxTokens = 16, kMoeMaxExperts = 256, kMoeMaxTopK = 8;
 constexpr int kMoeMaxActive = kMoeMaxTokens * kMoeMaxTopK;
 constexpr int kMoeMaxParts = 8;         // workgroups of a strip of the down layers
+// Blocks of a block row, in the mean over all layers.
+int moe_mean_blocks(const std::vector<const pivot_qfc_plan_t*>& layers);
 
 // One expert as the kernels see it: its two layers (0 gate/up, 1 down), and where a unit's activation goes in the down
 // layer's input.  whole > 0: every tile is kept, `whole` blocks in each block row, so that neither the blocks of a row nor
@@ -123,7 +125,7 @@ struct MoeRoute {
 struct MoeLaunch {
     const MoeExpert* experts; const void* router; int router_type; const float* router_bias; int renormalise;
     int E, top_k, D, F, F_pad, gather;                      // gather: whether any gate/up layer takes its columns in an order of its own
-    int bh[2], bw[2], gpk[2], zeros[2], nstrips[2], mean_kb[2];
+    int bh[2], bw[2], gpk[2], zeros[2], nstrips[2], down_blocks;   // down_blocks: of a block row, in the mean
     const int32_t* prow_down;
     const void* x; int64_t ldx; float* y; int64_t ldy; int tokens; int32_t* ids; float* weights;
     uint32_t* tickets; float* partials;                   // of the strips of the down layers
@@ -142,6 +144,7 @@ struct pivot_qfc_plan {
 
 struct pivot_moe_plan {
     std::vector<const pivot_qfc_plan_t*> gate_up, down;
+    int down_blocks = 0;                // moe_mean_blocks of the down layers
     int E = 0, top_k = 0, D = 0, F = 0, router_type = 0, renormalise = 0, gather = 0, device = -1;
     float eps = 0.f;
     char* dev_base = nullptr;

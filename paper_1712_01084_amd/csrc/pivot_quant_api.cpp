@@ -315,6 +315,7 @@ int pivot_moe_plan(const pivot_moe_desc* desc, const pivot_qfc_plan_t* const* ga
     if (!p) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
     p->gate_up.assign(gate_up, gate_up + E);
     p->down.assign(down, down + E);
+    p->down_blocks = moe_mean_blocks(p->down);
     p->E = E; p->top_k = k; p->D = D; p->F = F; p->router_type = desc->router_type; p->renormalise = desc->flags & PIVOT_MOE_RENORMALISE;
     p->device = device; p->eps = desc->norm_eps;
     if (device < 0) { set_error("host-only plan (device = -1) cannot run"); return PIVOT_E_NO_DEVICE; }
@@ -406,8 +407,8 @@ int pivot_moe_run(const pivot_moe_plan_t* plan, const void* x_dev, int xtype, in
     const QfcHost* hs[2] = {&plan->gate_up[0]->host, &plan->down[0]->host};
     for (int q = 0; q < 2; ++q) {
         L.bh[q] = hs[q]->d.bh; L.bw[q] = hs[q]->d.bw; L.gpk[q] = hs[q]->gpk; L.zeros[q] = hs[q]->has_zeros; L.nstrips[q] = hs[q]->M_pad / kQStrip;
-        L.mean_kb[q] = hs[q]->KB / hs[q]->nbr;
     }
+    L.down_blocks = plan->down_blocks;
     L.gather = plan->gather;
     L.experts = plan->experts; L.router = plan->router; L.router_type = plan->router_type; L.router_bias = plan->router_bias; L.renormalise = plan->renormalise;
     L.E = plan->E; L.top_k = plan->top_k; L.D = plan->D; L.F = plan->F; L.F_pad = hs[1]->K_pad; L.prow_down = plan->down[0]->dev.prow_pad;

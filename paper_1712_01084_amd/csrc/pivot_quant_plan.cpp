@@ -110,4 +110,10 @@ size_t qfc_partial_bytes(const QfcHost& h, int batch) {
     return h.max_parts > 1 ? align_up((size_t)h.nchunks * h.d.bh * batch * 4, 256) : 0;
 }
 
+int moe_mean_blocks(const std::vector<const pivot_qfc_plan_t*>& layers) {
+    int64_t blocks = 0, rows = 0;
+    for (const pivot_qfc_plan_t* p : layers) { blocks += p->host.KB; rows += p->host.nbr; }
+    return rows ? (int)(blocks / rows) : 0;
+}
+
 }  // namespace pivot
