@@ -9,6 +9,7 @@
 // trip, two reductions, stores.  Rows of up to 16384 columns are kept whole; 64x9203 fp32 into fp16 5.3 us.
 // The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
 // 10^5 would fall to the other side of the middle between two.
+#include <algorithm>
 #include <type_traits>
 
 #include "pivot_quant_core.h"
@@ -119,7 +120,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch 
     __shared__ double s_sum[NT / 64], s_most[NT / 64];
     extern __shared__ __align__(16) char s_row[];       // the output row, where it is put together there
     const int tid = threadIdx.x % TPR, lane = threadIdx.x & 63, wave = q_wave();
-    const long long row = (long long)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
+    const long long row = a.row0 + (long long)blockIdx.x * (NT / TPR) + threadIdx.x / TPR;
     if (TPR < 256 && row >= a.rows) return;             // (whole wavefronts: no barrier below for TPR = 64)
     const long long xo = row * a.ldx, ro = row * a.ldr, so = row * a.ldro, oo = row * a.ldo;
     const int es = Q8 ? 1 : (a.otype == PIVOT_F32 ? 4 : 2);
@@ -273,9 +274,14 @@ int norm_go(NormLaunch a) {
     auto go = [&](auto k, int per, int threads) {
         const size_t row = align_up((size_t)a.cols * (a.otype == PIVOT_Q8 ? 1 : elem_size(a.otype)), 16) * per;
         a.lds_rows = ORDER && row <= 60 * 1024;          // (longer rows: element by element)
-        hipLaunchKernelGGL(k, dim3((unsigned)(((long long)a.rows + per - 1) / per)), dim3(threads), a.lds_rows ? row : 0, st, a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
+        const long long blocks = ((long long)a.rows + per - 1) / per;
+        constexpr long long kMost = 1 << 21;             // (a launch has less than 2^32 threads)
+        for (long long b = 0; b < blocks; b += kMost) {
+            a.row0 = (int)(b * per);
+            hipLaunchKernelGGL(k, dim3((unsigned)std::min(kMost, blocks - b)), dim3(threads), a.lds_rows ? row : 0, st, a);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) { set_error("launch failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
+        }
         return PIVOT_OK;
     };
     const bool many = a.rows >= 512;                      // rows enough to fill the device with few threads each

@@ -85,7 +85,7 @@ int    launch_qfc(const QfcLaunch& L, std::string* describe = nullptr);
 struct NormLaunch {
     const void* x; int64_t ldx; const void* res; int64_t ldr; void* res_out; int64_t ldro; const float* weight;
     void* out; int64_t ldo; float* scale; const int32_t* order;   // order: [cols] out[c] = natural column order[c], or NULL
-    int xtype, rtype, otype, rows, cols; float eps; int lds_rows; void* stream;   // lds_rows: set by the launcher
+    int xtype, rtype, otype, rows, cols; float eps; int lds_rows, row0; void* stream;   // lds_rows, row0: set by the launcher
 };
 int launch_norm(const NormLaunch& L);
 
