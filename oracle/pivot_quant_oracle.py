@@ -113,8 +113,9 @@ def moe(x, router, bias, gate_up, down, top_k, renormalise):
     x, R = np.asarray(x, dtype=np.float64), np.asarray(router, dtype=np.float64)
     T, D = x.shape
     logits = x @ R.T + (0.0 if bias is None else np.asarray(bias, dtype=np.float64))
-    # a thread adds D / 256 products (8 at least), then 6 steps in a wavefront, 4 wavefronts, the bias
-    dl = (D / 256 + 8 + 12) * U * (np.abs(x) @ np.abs(R).T + (0.0 if bias is None else np.abs(np.where(np.isinf(bias), 0.0, bias)))).max(axis=1, keepdims=True)
+    # a lane adds every 64th eight products at most (one wavefront to a token): ceil(D / 512) * 8 roundings; then 6 steps in a
+    # wavefront, up to 16 wavefronts, the bias
+    dl = (8 * -(-D // 512) + 6 + 16 + 1) * U * (np.abs(x) @ np.abs(R).T + (0.0 if bias is None else np.abs(np.where(np.isinf(bias), 0.0, bias)))).max(axis=1, keepdims=True)
     ids, w = route(logits, top_k, renormalise)
     dw = w * (2 * dl + 80 * U)          # exponentials (2 units each), up to 70 additions, a division
     y, dy = np.zeros((T, D)), np.zeros((T, D))

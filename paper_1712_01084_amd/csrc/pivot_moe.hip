@@ -270,18 +270,14 @@ __global__ void __launch_bounds__(W * 64, 4) moe_up_kernel(MoeLaunch a, int vec)
         #pragma unroll
         for (int i = 0; i < 4; ++i) red[wave * N + (lane & 15) * (16 * RS) + 16 * r + 4 * (lane >> 4) + i] = acc[r][0][i];
     __syncthreads();
-    auto finish = [&](int m, int u, int to, int row, float g, float v) {
-        #pragma unroll
-        for (int w = 0; w < W; ++w) { g += red[w * N + m * 16 * RS + 2 * u]; v += red[w * N + m * 16 * RS + 2 * u + 1]; }
-        if (to >= 0) a.h[(size_t)row * a.F_pad + to] = g / (1.f + expf(-g)) * v;
-    };
     if (blockIdx.x == 0)                                 // the columns that fill up the down layer's last tile
         for (int i = tid; i < ntok * (a.F_pad - a.F); i += W * 64)
             a.h[(size_t)act.hrow[i / (a.F_pad - a.F)] * a.F_pad + a.F + i % (a.F_pad - a.F)] = 0.f;
-    if (em < ntok) finish(em, eu, dst, hrow, bg, bu);
-    for (int i = tid + W * 64; i < 8 * RS * ntok; i += W * 64) {
-        const int m = i / (8 * RS), u = i % (8 * RS);
-        finish(m, u, ex.hdst[strip * 8 + u], act.hrow[m], ex.bias[0][strip * 16 + 2 * u], ex.bias[0][strip * 16 + 2 * u + 1]);
+    static_assert(8 * RS * kMoeMaxTokens <= W * 64, "a thread has one unit of one token");
+    if (em < ntok && dst >= 0) {
+        #pragma unroll
+        for (int w = 0; w < W; ++w) { bg += red[w * N + em * 16 * RS + 2 * eu]; bu += red[w * N + em * 16 * RS + 2 * eu + 1]; }
+        a.h[(size_t)hrow * a.F_pad + dst] = bg / (1.f + expf(-bg)) * bu;
     }
 }
 
@@ -342,18 +338,17 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
     }
     __syncthreads();
     const int units = s_cum[n_act];
-    // what the end needs is asked for now: this thread's (first) output, its experts' biases
+    // what the end needs is asked for now: this thread's output, its experts' biases
+    static_assert(16 * kMoeMaxTokens <= W * 64, "a thread has one output");
     int e_dst = -1;
     float e_bias = 0.f;
-    auto bias_of = [&](int i) {
-        float s = 0.f;
+    if (tid < 16 * T) {
+        e_dst = a.prow_down[strip * 16 + tid % 16];
         for (int j = 0; j < a.top_k; ++j) {
-            const int e = a.route->sel[i / 16][j];
-            if (e >= 0) s = __builtin_fmaf(a.route->sel_w[i / 16][j], gload<float>(a.experts[e].bias[1] + strip * 16 + i % 16), s);
+            const int e = a.route->sel[tid / 16][j];
+            if (e >= 0) e_bias = __builtin_fmaf(a.route->sel_w[tid / 16][j], gload<float>(a.experts[e].bias[1] + strip * 16 + tid % 16), e_bias);
         }
-        return s;
-    };
-    if (tid < 16 * T) { e_dst = a.prow_down[strip * 16 + tid % 16]; e_bias = bias_of(tid); }
+    }
     char* xs = smem + wave * (kDownRows<NT> * ROW);
     // this lane's column: a token, its value or (second half of a single tile) its remainder
     const int n = NT == 1 ? (lane & 7) : (lane & 15), second = NT == 1 ? (lane >> 3) & 1 : 0;
@@ -491,7 +486,7 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
     };
     float* mine = a.partials + (size_t)strip * parts * 16 * T;
     if (parts > 1) {                                    // handed over as the pieces of a block row of a layer are
-        for (int i = tid; i < 16 * T; i += W * 64) agent_store(mine + blockIdx.y * 16 * T + i, sum_of(i));
+        if (tid < 16 * T) agent_store(mine + blockIdx.y * 16 * T + tid, sum_of(tid));
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (tid == 0) {
@@ -503,13 +498,11 @@ __global__ void __launch_bounds__(W * 64, 4) moe_down_kernel(MoeLaunch a) {
         __syncthreads();
         if (!s_last) return;
     }
-    for (int i = tid; i < 16 * T; i += W * 64) {
-        const int dst = i == tid ? e_dst : a.prow_down[strip * 16 + i % 16];
+    if (e_dst >= 0) {                                   // (of the first 16 T threads)
         float s = 0.f;
-        if (parts > 1) { for (int q = 0; q < parts; ++q) s += agent_load(mine + q * 16 * T + i); }
-        else s = sum_of(i);
-        s += i == tid ? e_bias : bias_of(i);
-        if (dst >= 0) a.y[i / 16 * a.ldy + dst] = s;
+        if (parts > 1) { for (int q = 0; q < parts; ++q) s += agent_load(mine + q * 16 * T + tid); }
+        else s = sum_of(tid);
+        a.y[tid / 16 * a.ldy + e_dst] = s + e_bias;
     }
 }
 
