@@ -521,7 +521,7 @@ int    pivot_qfc_kernel_name(const pivot_qfc_plan_t* plan, int xtype, int batch,
  *   scale      device, [rows] fp32; PIVOT_Q8 only
  *   order      a plan with K = cols: the rows of out are left in its block order, so that its run need not gather
  *              (PIVOT_QFC_X_BLOCK_ORDER); or NULL
- * rows >= 1, cols 1..65535.  Needs no workspace.
+ * rows >= 1, cols 1..65535.  Needs no workspace.  Runs on the device of `order`, without one on the current device.
  */
 typedef struct pivot_norm_args {
     const void* x; int64_t ldx;

@@ -7,6 +7,7 @@
 #include <cstring>
 #include <new>
 
+#include "pivot_device_guard.h"
 #include "pivot_internal.h"
 
 namespace pivot {
@@ -26,16 +27,6 @@ using namespace pivot;
     } while (0)
 
 namespace {
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) { ok = false; return; }
-        if (prev != dev && hipSetDevice(dev) != hipSuccess) ok = false;
-    }
-    ~DeviceGuard() { if (prev >= 0) (void)hipSetDevice(prev); }
-};
 
 struct Piece { const void* src; size_t bytes; void** dst; };
 

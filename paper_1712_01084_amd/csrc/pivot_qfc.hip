@@ -140,7 +140,6 @@ static QfcForm qfc_form(const QfcHost& h, int batch, bool as_it_lies, bool* copy
     const int strips = h.nchunks * h.strips();
     const size_t staged = h.units() * kQBlk * batch;                  // elements of x that the rows form stages
     QfcForm f{};
-    f.w = 8;
     f.nt = batch <= 16 ? 1 : (batch <= 32 ? 2 : 4);
     if (batch > 16) f.frag = 1;
     else if (as_it_lies) f.frag = batch > 8 && staged > ((size_t)1 << 24);

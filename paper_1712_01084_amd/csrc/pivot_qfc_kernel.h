@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(W * 64) qfc_frag_kernel(QfcArgs a) {
 }
 
 // The form a call takes: rows (frag = 0) or fragment, column tiles, strips per item, rows form: whether x is read as
-// it lies, wavefronts.
-struct QfcForm { int frag, nt, rs, fast, w; };
+// it lies; wavefronts of a workgroup.
+struct QfcForm { int frag, nt, rs, fast; static constexpr int w = 8; };
 
 inline size_t qfc_smem(const QfcForm& f, int batch, int row) {
     const size_t red = (size_t)f.w * 16 * f.rs * 16 * f.nt * 4;

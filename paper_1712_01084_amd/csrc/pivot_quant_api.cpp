@@ -4,25 +4,15 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <memory>
 #include <new>
 
+#include "pivot_device_guard.h"
 #include "pivot_quant.h"
 
 using namespace pivot;
 
 namespace {
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true, changed = false;
-    explicit DeviceGuard(int dev) {
-        if (hipGetDevice(&prev) != hipSuccess) { (void)hipGetLastError(); ok = false; return; }
-        if (prev == dev) return;
-        if (hipSetDevice(dev) == hipSuccess) changed = true;
-        else { (void)hipGetLastError(); ok = false; }
-    }
-    ~DeviceGuard() { if (changed) (void)hipSetDevice(prev); }
-};
 
 struct DeviceMemory {       // freed unless released
     char* p = nullptr;
@@ -162,7 +152,7 @@ int pivot_qfc_plan(const pivot_qfc_desc* desc, const uint8_t* codes, const void*
     if (out) *out = nullptr;
     if (!desc || !out) { set_error("desc and out are required"); return PIVOT_E_NULL; }
     if (!codes || !scales) { set_error("codes and scales are required"); return PIVOT_E_NULL; }
-    pivot_qfc_plan_t* p = new (std::nothrow) pivot_qfc_plan_t();
+    std::unique_ptr<pivot_qfc_plan_t> p(new (std::nothrow) pivot_qfc_plan_t());
     if (!p) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
     // (sizes that the builder refuses are not looked through)
     const int64_t groups = desc->M > 0 && desc->K > 0 && desc->group > 0 ? (int64_t)desc->M * (((int64_t)desc->K + desc->group - 1) / desc->group) : 0;
@@ -174,11 +164,10 @@ int pivot_qfc_plan(const pivot_qfc_desc* desc, const uint8_t* codes, const void*
     if (there) p->host.has_zeros = zeros != nullptr;
     if (rc == PIVOT_OK && desc->device >= 0) {
         p->device = desc->device;
-        try { rc = upload(p, codes, static_cast<const uint16_t*>(scales), zeros, bias); }
-        catch (const std::bad_alloc&) { set_error("out of host memory"); rc = PIVOT_E_ALLOC; }
+        rc = upload(p.get(), codes, static_cast<const uint16_t*>(scales), zeros, bias);
     }
-    if (rc != PIVOT_OK) { delete p; return rc; }
-    *out = p;
+    if (rc != PIVOT_OK) return rc;
+    *out = p.release();
     return PIVOT_OK;
 } catch (...) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
 
@@ -310,8 +299,7 @@ int pivot_moe_plan(const pivot_moe_desc* desc, const pivot_qfc_plan_t* const* ga
             if (u.prow_pad[2 * i] % 2 != 0 || u.prow_pad[2 * i + 1] != u.prow_pad[2 * i] + 1) { set_error("expert %d: gate_up's row permutation parts the gate and the up row of a unit", e); return PIVOT_E_UNSUPPORTED; }
         if (d.prow_pad != d0.prow_pad) { set_error("expert %d: the down layers must share one row permutation", e); return PIVOT_E_UNSUPPORTED; }
     }
-    struct Guard { pivot_moe_plan_t* p; ~Guard() { delete p; } } made{new (std::nothrow) pivot_moe_plan_t()};
-    pivot_moe_plan_t* p = made.p;
+    std::unique_ptr<pivot_moe_plan_t> p(new (std::nothrow) pivot_moe_plan_t());
     if (!p) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
     p->gate_up.assign(gate_up, gate_up + E);
     p->down.assign(down, down + E);
@@ -356,8 +344,7 @@ int pivot_moe_plan(const pivot_moe_desc* desc, const pivot_qfc_plan_t* const* ga
     if (rc == PIVOT_OK) rc = put(hdst_dev, hdst.data(), hdst.size() * 4);
     if (rc != PIVOT_OK) return rc;
     p->dev_base = mem.release();
-    made.p = nullptr;
-    *out = p;
+    *out = p.release();
     return PIVOT_OK;
 } catch (...) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
 
@@ -395,7 +382,7 @@ int pivot_moe_run(const pivot_moe_plan_t* plan, const void* x_dev, int xtype, in
     char* ws = static_cast<char*>(ws_dev);
     MoeLaunch L{};
     L.x = x_dev; L.ldx = ldx;
-    if (plan->norm_weight) {
+    if (plan->norm_weight) {                            // (into fp16, which is what the matrix instructions of the experts take)
         pivot_norm_args n{};
         n.x = x_dev; n.ldx = ldx; n.res = res_dev; n.ldr = ldx; n.res_out = res_dev; n.ldro = ldx; n.weight = plan->norm_weight;
         n.out = ws + s.x; n.ldo = (int64_t)align_up(plan->D, 8); n.xtype = xtype; n.rtype = xtype; n.otype = PIVOT_F16;
