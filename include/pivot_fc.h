@@ -553,8 +553,8 @@ int    pivot_norm_run(const pivot_norm_args* args, void* stream);
  *
  * A router_bias of -infinity switches an expert off.  A token with fewer than top_k experts left uses those (its
  * other ids are -1, their weights 0), one with none gets y = 0.  A token whose logits hold a NaN gets y = NaN.
- * Activations between the two layers are fp32; the down layer's products take 22 bits of one, or what 2^-50 of the
- * largest in its 128 columns leaves of it.
+ * Activations between the two layers are fp32; the down layer's products take one to within 2^-23 of it, or 2^-50 of the
+ * largest in its 128 columns.
  */
 typedef struct pivot_moe_plan pivot_moe_plan_t;
 #define PIVOT_MOE_RENORMALISE 1

@@ -126,9 +126,9 @@ def moe(x, router, bias, gate_up, down, top_k, renormalise):
         silu = g / (1.0 + np.exp(-g))
         h = silu * u
         # the slope of silu is below 1.1; an exponential, a sum, a division and a product, stored in fp32; as value and remainder
-        # in fp16 under a power of two by which the largest lies in [2^14, 2^15): half a step of each, 2^-11 * 2^-11, or half
-        # the remainder's subnormal step, 2^-25 / 2^11 beside 2^14
-        dh = (1.1 * dg * np.abs(u) + np.abs(silu) * du + dg * du * 1.1 + np.abs(h) * (8 * U + 2.0 ** -22) + 2.0 ** -149
+        # in fp16 under a power of two by which the largest lies in [2^14, 2^15): of an activation in [2^e, 2^(e+1)) the value
+        # leaves at most 2^(e-11), of that the remainder half a step, 2^(e-23), or half its subnormal step, 2^-25 / 2^11 beside 2^14
+        dh = (1.1 * dg * np.abs(u) + np.abs(silu) * du + dg * du * 1.1 + np.abs(h) * (8 * U + 2.0 ** -23) + 2.0 ** -149
               + 2.0 ** -50 * np.abs(h).max(axis=1, keepdims=True))
         W, A = dense_natural(dn)
         b = np.zeros(D) if dn["bias"] is None else np.asarray(dn["bias"], dtype=np.float64)

@@ -287,10 +287,10 @@ __global__ void __launch_bounds__(W * 64, 4) moe_up_kernel(MoeLaunch a, int vec)
 // 91).  NT = 2: values and remainders of h are two column tiles; NT = 1 (up to 8 tokens): columns 0-7 and 8-15 of one.
 //
 // A token's activations under a unit are staged by the sixteen lanes that load them as 2^s h = value + remainder / 2^11, both
-// fp16, s such that the largest of the unit's 128 lies in [2^14, 2^15); 2^-s multiplies the unit's sums.  Value and remainder
-// leave 2^-22 of an activation, or 2^-50 of the largest one (the remainder's last subnormal place) where that is more: less
-// than the 2^-23 that every addition of an fp32 sum of the products may cost, whatever the size of the activations.  A single
-// fp16 would leave 2^-11.
+// fp16, s such that the largest of the unit's 128 lies in [2^14, 2^15); 2^-s multiplies the unit's sums.  The remainder of an
+// activation in [2^e, 2^(e+1)) is at most half a step of the value, 2^(e-11), and half a step of the remainder 2^(e-23): the
+// pair is off by one step of fp32 at most, or by 2^-50 of the largest activation (half the remainder's subnormal step) where
+// that is more.  A single fp16 would be off by 2^-11.
 //
 // rows that a wavefront stages: at least the values and remainders of all tokens in one unit
 template <int NT> constexpr int kDownRows = 16 * NT;
