@@ -39,7 +39,7 @@ EXPORTS = [
     "pivot_mlp_workspace_bytes", "pivot_mlp_run", "pivot_mlp_kernel_name", "pivot_mlp_status", "pivot_mlp_status_word",
     "pivot_lstm_workspace_bytes", "pivot_lstm_run", "pivot_lstm_status", "pivot_lstm_status_word", "pivot_lstm_restore", "pivot_lstm_kernel_name",
     "pivot_dense_run", "pivot_csr_run", "pivot_null_run", "pivot_stream_read_run", "pivot_exchange_probe_run", "pivot_feedback_search",
-    "pivot_qfc_plan", "pivot_qfc_plan_host_view", "pivot_qfc_plan_destroy", "pivot_qfc_workspace_bytes", "pivot_qfc_run", "pivot_qfc_run_kernel_name", "pivot_qfc_kernel_name",
+    "pivot_qfc_plan", "pivot_qfc_plan_many", "pivot_qfc_plan_host_view", "pivot_qfc_plan_destroy", "pivot_qfc_workspace_bytes", "pivot_qfc_run", "pivot_qfc_run_kernel_name", "pivot_qfc_kernel_name",
     "pivot_norm_run", "pivot_moe_plan", "pivot_moe_plan_destroy", "pivot_moe_workspace_bytes", "pivot_moe_run",
 ]
 
@@ -153,6 +153,7 @@ def lib():
     L.pivot_feedback_search.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, C.POINTER(C.c_double)]
     L.pivot_csr_run.argtypes = [vp, vp, vp, i32, i32, i64, vp, vp, vp, i32, vp]
     L.pivot_qfc_plan.argtypes = [C.POINTER(pivot_qfc_desc), vp, vp, vp, vp, vp, vp, vp, C.POINTER(vp)]
+    L.pivot_qfc_plan_many.argtypes = [C.c_int, C.POINTER(pivot_qfc_desc)] + [C.POINTER(vp)] * 8
     L.pivot_qfc_plan_host_view.argtypes = [vp, C.POINTER(pivot_qfc_view)]
     L.pivot_qfc_plan_destroy.argtypes = [vp]
     L.pivot_qfc_plan_destroy.restype = None
@@ -402,11 +403,9 @@ def _array(a, dtype, shape, name):
     return a
 
 
-def pivot_qfc_plan(M, K, bh, bw, group, codes, scales, zeros=None, tile_mask=None, prow=None, pcol=None, bias=None, *,
-                   act=PIVOT_ACT_NONE, chunk_blocks=0, device=-1, flags=0):
-    """Host numpy arrays in (codes: [M][ceil(K/2)] bytes, scales: [M][ceil(K/group)] fp16), opaque plan handle out.  With
-    PIVOT_QFC_WEIGHTS_ON_DEVICE among the flags codes, scales, zeros and bias are device addresses of such arrays."""
-    d = pivot_qfc_desc(M, K, bh, bw, group, act, chunk_blocks, device, flags)
+def _qfc_layer(M, K, bh, bw, group, codes, scales, zeros=None, tile_mask=None, prow=None, pcol=None, bias=None, *, act=PIVOT_ACT_NONE,
+               chunk_blocks=0, device=-1, flags=0):
+    """Descriptor and arrays of a layer, in the order of the library's arguments."""
     if min(M, K, bh, bw, group) > 0:      # the library refuses the rest
         ng = -(-K // group)
         if not flags & PIVOT_QFC_WEIGHTS_ON_DEVICE:
@@ -416,10 +415,34 @@ def pivot_qfc_plan(M, K, bh, bw, group, codes, scales, zeros=None, tile_mask=Non
             bias = _array(bias, np.float32, (M,), "bias")
         tile_mask = _array(tile_mask, np.uint8, (-(-M // bh), -(-K // bw)), "tile_mask")
         prow, pcol = _array(prow, np.int32, (M,), "prow"), _array(pcol, np.int32, (K,), "pcol")
+    return pivot_qfc_desc(M, K, bh, bw, group, act, chunk_blocks, device, flags), (codes, scales, zeros, tile_mask, prow, pcol, bias)
+
+
+def _address(a):
+    """Of an array, or an address as it is."""
+    return a if a is None or isinstance(a, int) else a.__array_interface__["data"][0]
+
+
+def pivot_qfc_plan(M, K, bh, bw, group, codes, scales, zeros=None, tile_mask=None, prow=None, pcol=None, bias=None, *,
+                   act=PIVOT_ACT_NONE, chunk_blocks=0, device=-1, flags=0):
+    """Host numpy arrays in (codes: [M][ceil(K/2)] bytes, scales: [M][ceil(K/group)] fp16), opaque plan handle out.  With
+    PIVOT_QFC_WEIGHTS_ON_DEVICE among the flags codes, scales, zeros and bias are device addresses of such arrays."""
+    d, arrays = _qfc_layer(M, K, bh, bw, group, codes, scales, zeros, tile_mask, prow, pcol, bias, act=act, chunk_blocks=chunk_blocks,
+                           device=device, flags=flags)
     out = C.c_void_p()
-    weights = [w if isinstance(w, int) else _np_ptr(w) for w in (codes, scales, zeros, bias)]
-    _check(lib().pivot_qfc_plan(C.byref(d), *weights[:3], _np_ptr(tile_mask), _np_ptr(prow), _np_ptr(pcol), weights[3], C.byref(out)))
+    _check(lib().pivot_qfc_plan(C.byref(d), *[_address(a) for a in arrays], C.byref(out)))
     return out
+
+
+def pivot_qfc_plan_many(layers, *, device=-1, flags=0):
+    """The plans of several layers, made at once.  Each is a dict of pivot_qfc_plan's arguments but device and flags."""
+    layers = [_qfc_layer(device=device, flags=flags, **layer) for layer in layers]
+    n = len(layers)
+    descs = (pivot_qfc_desc * max(n, 1))(*[d for d, _ in layers])
+    lists = [(C.c_void_p * max(n, 1))(*[_address(arrays[i]) for _, arrays in layers]) for i in range(7)]
+    out = (C.c_void_p * max(n, 1))()
+    _check(lib().pivot_qfc_plan_many(n, descs, *lists, out))
+    return [C.c_void_p(h) for h in out]
 
 
 def pivot_qfc_plan_host_view(plan):

@@ -88,20 +88,17 @@ __global__ void __launch_bounds__(256) qfc_bias_kernel(float* bias_p, const floa
 }
 
 int launch_qfc_pack(const QfcHost& h, const QfcDev& d, const uint8_t* raw_codes, const uint16_t* raw_scales, const uint8_t* raw_zeros,
-                    const float* raw_bias) {
+                    const float* raw_bias, int32_t* bad) {
     const QfcPack p{reinterpret_cast<u32x4*>(d.codes), d.scales, d.zeros, raw_codes, raw_scales, raw_zeros, d.row_of_kb, d.kb_ptr, d.pieces,
-                    d.bad, h.d.M, h.d.K, h.d.bh, h.d.bw, h.d.group, h.gpk};
+                    bad, h.d.M, h.d.K, h.d.bh, h.d.bw, h.d.group, h.gpk};
     constexpr int kSlice = 1 << 24;                             // (a launch has less than 2^32 threads)
     for (int kb = 0; kb < h.KB; kb += kSlice) {
         const int end = std::min(h.KB, kb + kSlice);
         hipLaunchKernelGGL(qfc_pack_kernel, dim3((end - kb + 3) / 4, h.strips()), dim3(256), 0, nullptr, p, kb, end);
     }
     if (raw_bias) hipLaunchKernelGGL(qfc_bias_kernel, dim3((h.M_pad + 255) / 256), dim3(256), 0, nullptr, d.bias_p, raw_bias, d.prow_pad, h.M_pad);
-    hipError_t e = hipGetLastError();
-    int32_t zero_above_15 = 0;
-    if (e == hipSuccess) e = raw_zeros ? hipMemcpy(&zero_above_15, d.bad, sizeof(int32_t), hipMemcpyDeviceToHost) : hipStreamSynchronize(nullptr);
-    if (e != hipSuccess) { (void)hipGetLastError(); set_error("laying out the weights failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
-    if (zero_above_15) { set_error("a zero point is above 15"); return PIVOT_E_SHAPE; }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) { set_error("laying out the weights failed: %s", hipGetErrorString(e)); return PIVOT_E_HIP; }
     return PIVOT_OK;
 }
 

@@ -9,6 +9,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <memory>
 #include <string>
 #include <vector>
 
@@ -48,7 +49,7 @@ struct QfcHost {
 };
 
 struct QfcDev {
-    char* base = nullptr;
+    std::shared_ptr<char> memory;       // freed with the last plan made in the same call
     void*  codes = nullptr;             // [units][64 lanes] 16 bytes; units of block row i: strip-major
     uint16_t* scales = nullptr;         // [units][4 quarters of the strip][gpk][4 rows] fp16
     uint8_t* zeros = nullptr;           // [units][16 rows][gpk], or NULL
@@ -60,15 +61,14 @@ struct QfcDev {
     int32_t* invpcol = nullptr;         // [K]
     float*   bias_p = nullptr;
     int32_t* row_of_kb = nullptr;       // [KB] the block row of a block (laying out)
-    int32_t* bad = nullptr;             // (laying out) whether a zero point is above 15
 };
 
 int  build_qfc_host(const pivot_qfc_desc& d, const uint8_t* zeros, int64_t groups, const uint8_t* tile_mask, const int32_t* prow,
                     const int32_t* pcol, const float* bias, QfcHost& h);
-// Lays the codes and scales out on the device, and waits for it; raw_*: the caller's arrays, there already (raw_bias NULL:
-// bias_p stands).
+// Lays the codes and scales out on the device, on the default stream; raw_*: the caller's arrays, there already (raw_bias NULL:
+// bias_p stands); *bad is set where a zero point is above 15.
 int  launch_qfc_pack(const QfcHost& h, const QfcDev& d, const uint8_t* raw_codes, const uint16_t* raw_scales,
-                     const uint8_t* raw_zeros, const float* raw_bias);
+                     const uint8_t* raw_zeros, const float* raw_bias, int32_t* bad);
 
 struct QfcLaunch {
     const QfcHost* h; const QfcDev* d;

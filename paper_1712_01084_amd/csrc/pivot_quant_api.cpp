@@ -6,9 +6,14 @@
 #include <cstring>
 #include <memory>
 #include <new>
+#include <string>
 
 #include "pivot_device_guard.h"
 #include "pivot_quant.h"
+
+namespace pivot {
+const char* last_error();
+}
 
 using namespace pivot;
 
@@ -46,70 +51,95 @@ bool on_device(const void* p, int device) {
     return at.type == hipMemoryTypeDevice && at.device == device;
 }
 
-// Weights and index arrays of a plan in one allocation, the index arrays in one copy.  Weights in host memory pass through a
-// second allocation that is freed again.
-int upload(pivot_qfc_plan_t* p, const uint8_t* codes, const uint16_t* scales, const uint8_t* zeros, const float* bias) {
-    const QfcHost& h = p->host;
-    QfcDev& d = p->dev;
-    const bool there = h.d.flags & PIVOT_QFC_WEIGHTS_ON_DEVICE;
-    DeviceGuard g(p->device);
-    if (!g.ok) { set_error("cannot select device %d", p->device); return PIVOT_E_HIP; }
-    if (there)
-        for (const void* q : {(const void*)codes, (const void*)scales, (const void*)zeros, (const void*)bias})
-            if (q && !on_device(q, p->device)) { set_error("PIVOT_QFC_WEIGHTS_ON_DEVICE: codes, scales, zeros and bias must be memory of device %d", p->device); return PIVOT_E_UNSUPPORTED; }
-    std::vector<int32_t> row_of_kb(h.KB);
-    for (int i = 0; i < h.nbr; ++i) std::fill(row_of_kb.begin() + h.kb_ptr[i], row_of_kb.begin() + h.kb_ptr[i + 1], i);
-    const int32_t none = 0;
-    const size_t units = h.units(), ns = units * h.gpk * kQStrip;
+// One plan on its way to the device: where its arrays lie in the allocation, and the caller's weights.
+struct Upload {
+    pivot_qfc_plan_t* p;
+    const uint8_t* codes; const uint16_t* scales; const uint8_t* zeros; const float* bias;
+    std::vector<int32_t> row_of_kb;
     struct Piece { const void* src; size_t bytes; void** dst; };
-    const Piece pieces[] = {
-        {nullptr, units * kQUnitBytes, &d.codes},
-        {nullptr, ns * 2, (void**)&d.scales},
-        {nullptr, h.has_zeros ? ns : 0, (void**)&d.zeros},
-        {h.kb_ptr.data(), h.kb_ptr.size() * 4, (void**)&d.kb_ptr},
-        {h.pieces.data(), h.pieces.size() * 4, (void**)&d.pieces},
-        {h.chunks.data(), h.chunks.size() * 4, (void**)&d.chunks},
-        {h.prow_pad.data(), h.prow_pad.size() * 4, (void**)&d.prow_pad},
-        {h.pcol_pad.data(), h.pcol_pad.size() * 4, (void**)&d.pcol_pad},
-        {h.invpcol.data(), h.invpcol.size() * 4, (void**)&d.invpcol},
-        {h.bias_p.data(), h.bias_p.size() * 4, (void**)&d.bias_p},
-        {row_of_kb.data(), row_of_kb.size() * 4, (void**)&d.row_of_kb},
-        {&none, sizeof(none), (void**)&d.bad},
-    };
-    constexpr int kLaidOut = 3;                         // the pieces that are made there; behind them those that are copied
-    size_t total = 0, copied_from = 0;
-    for (const Piece& q : pieces) {
-        if (&q == pieces + kLaidOut) copied_from = total;
-        total += align_up(q.bytes + 1, 256);
+    std::vector<Piece> copied, laid_out;
+    void arrange() {
+        const QfcHost& h = p->host;
+        QfcDev& d = p->dev;
+        row_of_kb.resize(h.KB);
+        for (int i = 0; i < h.nbr; ++i) std::fill(row_of_kb.begin() + h.kb_ptr[i], row_of_kb.begin() + h.kb_ptr[i + 1], i);
+        const size_t units = h.units(), ns = units * h.gpk * kQStrip;
+        copied = {
+            {h.kb_ptr.data(), h.kb_ptr.size() * 4, (void**)&d.kb_ptr},
+            {h.pieces.data(), h.pieces.size() * 4, (void**)&d.pieces},
+            {h.chunks.data(), h.chunks.size() * 4, (void**)&d.chunks},
+            {h.prow_pad.data(), h.prow_pad.size() * 4, (void**)&d.prow_pad},
+            {h.pcol_pad.data(), h.pcol_pad.size() * 4, (void**)&d.pcol_pad},
+            {h.invpcol.data(), h.invpcol.size() * 4, (void**)&d.invpcol},
+            {h.bias_p.data(), h.bias_p.size() * 4, (void**)&d.bias_p},
+            {row_of_kb.data(), row_of_kb.size() * 4, (void**)&d.row_of_kb},
+        };
+        laid_out = {{nullptr, units * kQUnitBytes, &d.codes}, {nullptr, ns * 2, (void**)&d.scales}};
+        if (h.has_zeros) laid_out.push_back({nullptr, ns, (void**)&d.zeros});
     }
+    static size_t room(const Piece& q) { return align_up(q.bytes + 1, 256); }
+};
+
+// Plans of one device, weights and index arrays of all of them in one allocation, the index arrays in one copy.  Weights in host
+// memory pass through a second allocation, large enough for one plan, that is freed again.
+int upload(std::vector<Upload>& ups, bool there) {
+    const int device = ups[0].p->device;
+    DeviceGuard g(device);
+    if (!g.ok) { set_error("cannot select device %d", device); return PIVOT_E_HIP; }
+    size_t image_bytes = 256, total = 0, most_raw = 0;      // the image begins with the word that a bad zero point sets
+    for (Upload& u : ups) {
+        const QfcHost& h = u.p->host;
+        if (there)
+            for (const void* q : {(const void*)u.codes, (const void*)u.scales, (const void*)u.zeros, (const void*)u.bias})
+                if (q && !on_device(q, device)) { set_error("PIVOT_QFC_WEIGHTS_ON_DEVICE: codes, scales, zeros and bias must be memory of device %d", device); return PIVOT_E_UNSUPPORTED; }
+        u.arrange();
+        for (const Upload::Piece& q : u.copied) image_bytes += Upload::room(q);
+        for (const Upload::Piece& q : u.laid_out) total += Upload::room(q);
+        const size_t groups = (size_t)h.d.M * ((h.d.K + h.d.group - 1) / h.d.group);
+        if (h.KB > 0) most_raw = std::max(most_raw, align_up((size_t)h.d.M * ((h.d.K + 1) / 2), 256) + align_up(groups * 2, 256) + groups);
+    }
+    total += image_bytes;
+    std::vector<char> image(image_bytes);
     DeviceMemory mem, raw;
     int rc = mem.get(total);
+    if (rc == PIVOT_OK && !there && most_raw) rc = raw.get(most_raw);
     if (rc != PIVOT_OK) return rc;
-    std::vector<char> image(total - copied_from);
-    size_t off = 0;
-    for (const Piece& q : pieces) {
-        *q.dst = mem.p + off;
-        if (off >= copied_from && q.bytes) memcpy(image.data() + (off - copied_from), q.src, q.bytes);
-        off += align_up(q.bytes + 1, 256);
-    }
-    if (!h.has_zeros) d.zeros = nullptr;
-    rc = put(mem.p + copied_from, image.data(), image.size());
-    if (rc == PIVOT_OK && !there) {
-        const size_t code_bytes = (size_t)h.d.M * ((h.d.K + 1) / 2), ngroups = (size_t)h.d.M * ((h.d.K + h.d.group - 1) / h.d.group);
-        const size_t o1 = align_up(code_bytes, 256), o2 = o1 + align_up(ngroups * 2, 256);
-        if (h.KB > 0) {
-            rc = raw.get(o2 + ngroups);
-            if (rc == PIVOT_OK) rc = put(raw.p, codes, code_bytes);
-            if (rc == PIVOT_OK) rc = put(raw.p + o1, scales, ngroups * 2);
-            if (rc == PIVOT_OK && zeros) rc = put(raw.p + o2, zeros, ngroups);
-            codes = reinterpret_cast<const uint8_t*>(raw.p);
-            scales = reinterpret_cast<const uint16_t*>(raw.p + o1);
-            zeros = reinterpret_cast<const uint8_t*>(raw.p + o2);
+    int32_t* bad = reinterpret_cast<int32_t*>(mem.p);
+    size_t off = 256;
+    for (Upload& u : ups)
+        for (const Upload::Piece& q : u.copied) {
+            if (q.bytes) memcpy(image.data() + off, q.src, q.bytes);
+            *q.dst = mem.p + off;
+            off += Upload::room(q);
         }
+    for (Upload& u : ups)
+        for (const Upload::Piece& q : u.laid_out) {
+            *q.dst = mem.p + off;
+            off += Upload::room(q);
+        }
+    rc = put(mem.p, image.data(), image.size());
+    for (Upload& u : ups) {
+        const QfcHost& h = u.p->host;
+        if (rc == PIVOT_OK && !there && h.KB > 0) {
+            if (const hipError_t e = hipStreamSynchronize(nullptr); e != hipSuccess) return hip_error("laying out the weights", e);   // the plan before, from the same memory
+            const size_t code_bytes = (size_t)h.d.M * ((h.d.K + 1) / 2), groups = (size_t)h.d.M * ((h.d.K + h.d.group - 1) / h.d.group);
+            const size_t o1 = align_up(code_bytes, 256), o2 = o1 + align_up(groups * 2, 256);
+            rc = put(raw.p, u.codes, code_bytes);
+            if (rc == PIVOT_OK) rc = put(raw.p + o1, u.scales, groups * 2);
+            if (rc == PIVOT_OK && u.zeros) rc = put(raw.p + o2, u.zeros, groups);
+            u.codes = reinterpret_cast<const uint8_t*>(raw.p);
+            u.scales = reinterpret_cast<const uint16_t*>(raw.p + o1);
+            if (u.zeros) u.zeros = reinterpret_cast<const uint8_t*>(raw.p + o2);
+        }
+        if (rc == PIVOT_OK) rc = launch_qfc_pack(h, u.p->dev, u.codes, u.scales, u.zeros, there ? u.bias : nullptr, bad);
     }
-    if (rc == PIVOT_OK) rc = launch_qfc_pack(h, d, codes, scales, zeros, there ? bias : nullptr);
-    if (rc != PIVOT_OK) { d = QfcDev{}; return rc; }
-    d.base = mem.release();
+    int32_t zero_above_15 = 0;
+    const hipError_t e = hipMemcpy(&zero_above_15, bad, sizeof(int32_t), hipMemcpyDeviceToHost);      // waits for all of it
+    if (rc == PIVOT_OK && e != hipSuccess) rc = hip_error("laying out the weights", e);
+    if (rc == PIVOT_OK && zero_above_15) { set_error("a zero point is above 15"); rc = PIVOT_E_SHAPE; }
+    if (rc != PIVOT_OK) return rc;
+    const std::shared_ptr<char> shared(mem.release(), [device](char* p) { DeviceGuard g(device); (void)hipFree(p); });
+    for (Upload& u : ups) u.p->dev.memory = shared;
     return PIVOT_OK;
 }
 
@@ -147,29 +177,54 @@ MoeScratch moe_scratch(const pivot_moe_plan_t* p, int tokens) {
 
 extern "C" {
 
-int pivot_qfc_plan(const pivot_qfc_desc* desc, const uint8_t* codes, const void* scales, const uint8_t* zeros, const uint8_t* tile_mask,
-                   const int32_t* prow, const int32_t* pcol, const float* bias, pivot_qfc_plan_t** out) try {
-    if (out) *out = nullptr;
-    if (!desc || !out) { set_error("desc and out are required"); return PIVOT_E_NULL; }
-    if (!codes || !scales) { set_error("codes and scales are required"); return PIVOT_E_NULL; }
-    std::unique_ptr<pivot_qfc_plan_t> p(new (std::nothrow) pivot_qfc_plan_t());
-    if (!p) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
-    // (sizes that the builder refuses are not looked through)
-    const int64_t groups = desc->M > 0 && desc->K > 0 && desc->group > 0 ? (int64_t)desc->M * (((int64_t)desc->K + desc->group - 1) / desc->group) : 0;
-    const bool there = desc->flags & PIVOT_QFC_WEIGHTS_ON_DEVICE;      // (what lies there is not read here)
-    int rc = PIVOT_OK;
-    if (there && desc->device < 0) { set_error("PIVOT_QFC_WEIGHTS_ON_DEVICE needs a device"); rc = PIVOT_E_NO_DEVICE; }
-    if (there && (!aligned_to(scales, 2) || !aligned_to(bias, 4))) { set_error("scales and bias must be aligned to their type"); rc = PIVOT_E_SHAPE; }
-    if (rc == PIVOT_OK) rc = build_qfc_host(*desc, there ? nullptr : zeros, groups, tile_mask, prow, pcol, there ? nullptr : bias, p->host);
-    if (there) p->host.has_zeros = zeros != nullptr;
-    if (rc == PIVOT_OK && desc->device >= 0) {
-        p->device = desc->device;
-        rc = upload(p.get(), codes, static_cast<const uint16_t*>(scales), zeros, bias);
+int pivot_qfc_plan_many(int n, const pivot_qfc_desc* descs, const uint8_t* const* codes, const void* const* scales,
+                        const uint8_t* const* zeros, const uint8_t* const* tile_mask, const int32_t* const* prow, const int32_t* const* pcol,
+                        const float* const* bias, pivot_qfc_plan_t** out) try {
+    if (n < 1) { set_error("n must be positive"); return PIVOT_E_SHAPE; }
+    if (out) std::fill(out, out + n, nullptr);
+    if (!descs || !out) { set_error("desc and out are required"); return PIVOT_E_NULL; }
+    const int device = descs[0].device;
+    const bool there = descs[0].flags & PIVOT_QFC_WEIGHTS_ON_DEVICE;      // (what lies there is not read here)
+    std::vector<std::unique_ptr<pivot_qfc_plan_t>> plans;
+    std::vector<Upload> ups(n);
+    auto build = [&](int i) -> int {
+        const pivot_qfc_desc& d = descs[i];
+        auto of = [i](auto* list) { return list ? list[i] : nullptr; };
+        Upload& u = ups[i];
+        u.codes = of(codes); u.scales = static_cast<const uint16_t*>(of(scales)); u.zeros = of(zeros); u.bias = of(bias);
+        if (!u.codes || !u.scales) { set_error("codes and scales are required"); return PIVOT_E_NULL; }
+        if (d.device != device || d.flags != descs[0].flags) { set_error("device and flags must be the same for all"); return PIVOT_E_UNSUPPORTED; }
+        if (there && device < 0) { set_error("PIVOT_QFC_WEIGHTS_ON_DEVICE needs a device"); return PIVOT_E_NO_DEVICE; }
+        if (there && (!aligned_to(u.scales, 2) || !aligned_to(u.bias, 4))) { set_error("scales and bias must be aligned to their type"); return PIVOT_E_SHAPE; }
+        // (sizes that the builder refuses are not looked through)
+        const int64_t groups = d.M > 0 && d.K > 0 && d.group > 0 ? (int64_t)d.M * (((int64_t)d.K + d.group - 1) / d.group) : 0;
+        plans.push_back(std::make_unique<pivot_qfc_plan_t>());
+        u.p = plans.back().get();
+        u.p->device = device;
+        const int rc = build_qfc_host(d, there ? nullptr : u.zeros, groups, of(tile_mask), of(prow), of(pcol), there ? nullptr : u.bias, u.p->host);
+        if (there) u.p->host.has_zeros = u.zeros != nullptr;
+        return rc;
+    };
+    for (int i = 0; i < n; ++i) {
+        const int rc = build(i);
+        if (rc != PIVOT_OK) {
+            const std::string why = last_error();
+            if (n > 1) set_error("layer %d: %s", i, why.c_str());
+            return rc;
+        }
     }
-    if (rc != PIVOT_OK) return rc;
-    *out = p.release();
+    if (device >= 0) {
+        const int rc = upload(ups, there);
+        if (rc != PIVOT_OK) return rc;
+    }
+    for (int i = 0; i < n; ++i) out[i] = plans[i].release();
     return PIVOT_OK;
 } catch (...) { set_error("out of host memory"); return PIVOT_E_ALLOC; }
+
+int pivot_qfc_plan(const pivot_qfc_desc* desc, const uint8_t* codes, const void* scales, const uint8_t* zeros, const uint8_t* tile_mask,
+                   const int32_t* prow, const int32_t* pcol, const float* bias, pivot_qfc_plan_t** out) {
+    return pivot_qfc_plan_many(1, desc, &codes, &scales, &zeros, &tile_mask, &prow, &pcol, &bias, out);
+}
 
 int pivot_qfc_plan_host_view(const pivot_qfc_plan_t* plan, pivot_qfc_view* v) {
     if (!plan || !v) { set_error("plan and view are required"); return PIVOT_E_NULL; }
@@ -183,11 +238,6 @@ int pivot_qfc_plan_host_view(const pivot_qfc_plan_t* plan, pivot_qfc_view* v) {
 }
 
 void pivot_qfc_plan_destroy(pivot_qfc_plan_t* plan) {
-    if (!plan) return;
-    if (plan->dev.base) {
-        DeviceGuard g(plan->device);
-        (void)hipFree(plan->dev.base);
-    }
     delete plan;
 }
 
