@@ -155,13 +155,13 @@ class _State:
             L["t_" + k] = torch.from_numpy(L[k]).cuda().long()
         return L
 
-    def plan(self, L):
+    def plans(self, layers):
         from paper_1712_01084_amd import binding as B
-        codes, scales, zeros, bias = (None if L[k] is None else L[k].data_ptr() for k in ("codes", "scales", "zeros", "bias"))
-        p = B.pivot_qfc_plan(L["M"], L["K"], L["bh"], L["bw"], L["group"], codes, scales, zeros, L["mask"], L["prow"], L["pcol"], bias,
-                             act=L["act"], device=0, flags=B.PIVOT_QFC_WEIGHTS_ON_DEVICE)
-        self.free.append((B.pivot_qfc_plan_destroy, p))
-        return p
+        ps = B.pivot_qfc_plan_many([dict({k: L[k] for k in ("M", "K", "bh", "bw", "group", "act", "prow", "pcol")}, tile_mask=L["mask"],
+                                         **{k: None if L[k] is None else L[k].data_ptr() for k in ("codes", "scales", "zeros", "bias")})
+                                    for L in layers], device=0, flags=B.PIVOT_QFC_WEIGHTS_ON_DEVICE)
+        self.free += [(B.pivot_qfc_plan_destroy, p) for p in ps]
+        return ps
 
     def workspace(self, nbytes):
         from paper_1712_01084_amd import binding as B
@@ -182,7 +182,7 @@ def _prepare_qfc(c, seed):
     s.y = torch.zeros(c["batch"], c["M"], device="cuda")
     if own:                       # a program lays its weights out once
         from paper_1712_01084_amd import binding as B
-        s.p = s.plan(s.layer_)
+        s.p, = s.plans([s.layer_])
         s.workspace(B.pivot_qfc_workspace_bytes(s.p, c["batch"]))
     return s
 
@@ -201,7 +201,7 @@ def _prepare_norm(c, seed):
     s.p = None
     if own and c["perm"]:         # the layer whose input the rows become: its column permutation is the order they are left in
         z = dict(bh=16, bw=32, group=32, kept=0.0, zeros=False)
-        s.p = s.plan(s.layer(16, cols, z, False, pcol=s.pcol))
+        s.p, = s.plans([s.layer(16, cols, z, False, pcol=s.pcol)])
     return s
 
 
@@ -218,8 +218,8 @@ def _prepare_moe(c, seed):
     s.weights = torch.zeros(c["tokens"], c["top_k"], device="cuda")
     if own:
         from paper_1712_01084_amd import binding as B
-        s.p = B.pivot_moe_plan([s.plan(L) for L in s.gate_up], [s.plan(L) for L in s.down], c["top_k"], s.router.cpu().numpy(),
-                               renormalise=c["renorm"])
+        ps = s.plans(s.gate_up + s.down)
+        s.p = B.pivot_moe_plan(ps[:E], ps[E:], c["top_k"], s.router.cpu().numpy(), renormalise=c["renorm"])
         s.free.append((B.pivot_moe_plan_destroy, s.p))
         s.workspace(B.pivot_moe_workspace_bytes(s.p, c["tokens"]))
         s.gate_up = s.down = None
