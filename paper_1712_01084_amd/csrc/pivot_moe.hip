@@ -10,10 +10,11 @@
 //
 // The weights of an expert in use are read once, whatever the number of its tokens.
 //
-// Us in a replayed graph, router / up / down: 1 token through 2 of 8 experts of 4096-8192-4096 (104 MB) 38.2 = 5 / 17.5 / 16.5,
-// reading alone 14.5 and 8.4 for the two layers; 16 tokens through 51 of 64 experts of 2048-1408-2048 (242 MB) 86 = 9 / 43 / 42,
-// reading alone 33 and 17; 4 tokens through 6.5 of 16 pruned experts 28.1 = 5 / 13.5 / 10.5, where the trips from the
-// router's list to the first weights count, four or five before each of the two layers streams.
+// Us in a replayed graph, router / up / down: 1 token through 2 of 8 experts of 4096-8192-4096 (104 MB) 39 = 5 / 17 / 17,
+// reading alone 14.5 and 8.4 for the two layers; 16 tokens through 51 of 64 experts of 2048-1408-2048 (242 MB) 89 = 9 / 42 / 44,
+// reading alone 33 and 17; 4 tokens through 6.5 of 16 pruned experts 28.3 = 5 / 13 / 11, where the trips from the
+// router's list to the first weights count, four or five before each of the two layers streams.  In the down layers the vector
+// units are busy 71 and 76 % of the time (dequantising, and the activations into two fp16 numbers), in the gate/up layers 62 and 66.
 #include <algorithm>
 #include <type_traits>
 

@@ -4,9 +4,11 @@
 //
 // TPR threads share a row, eight neighbouring columns each at a time, and keep weight * h (or both) in registers between the two
 // passes (sum of squares and largest weight * h, then the outputs); what of a row does not fit there is read a second
-// time.  8192x4096, residual and output fp16: 51 us = 5.2 TB/s, what a copy reaches; fp32 into 8 bits 84 us = 5.2; fp16 into 8
-// bits 62 us = 3.8, bound by the 64-bit operations.  One row of 4096: 3.1 us, 3.6 into 8 bits, 5.4 in block order: launch, one
-// trip, two reductions, stores.  Rows of up to 16384 columns are kept whole; 64x9203 fp32 into fp16 5.3 us.
+// time.  8192x4096, residual and output fp16: 51 us = 5.2 TB/s, what a copy reaches; fp32 into fp32 95 us = 5.6; fp32 into 8
+// bits 84 us = 5.2; fp16 into 8 bits 61 us = 3.8, where the vector units are busy 68 % of the time with 45 instructions a column.
+// One row of 4096: 3.2 us, 3.5 into 8 bits, 5.2 in block order: launch, one trip, two reductions, stores.  Rows of up to 16384
+// columns are kept whole, their loads out together (64x9203 fp32 into fp16 5.8 -> 5.3 us, 2048x16000 fp16 into 8 bits 69 -> 64,
+// but 8192x4096 fp32 into 8 bits 81 -> 84).  In block order 8192x4096 fp16 into fp16 takes 104 us, into 8 bits 102.
 // The 8-bit codes depend on weight * h / max alone, which is computed in 64 bits: in 32 bits about one code in
 // 10^5 would fall to the other side of the middle between two.
 #include <algorithm>
@@ -111,7 +113,7 @@ __device__ __forceinline__ int code_of(double v, double inv) {
 
 // WIDE: h and weight * h in 64 bits, for 8-bit rows and where an input is fp32: its sums and products may leave the range of
 // fp32 where the output does not.  Rows of fp16 stay far inside it as long as h / rms is formed first; 64 bits would cost them
-// more than the memory hides (8192x4096 fp16 into fp16 53 -> 58 us, 100000x300 83 -> 106; fp32 into fp32 93 -> 95).
+// more than the memory hides (8192x4096 fp16 into fp16 51 -> 58 us, 100000x300 83 -> 106; fp32 into fp32 93 -> 95).
 template <bool Q8, bool WIDE, bool ORDER, int TPR, int KEEP>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(NormLaunch a) {
     constexpr int NT = TPR < 256 ? 256 : TPR, NW = TPR / 64;

@@ -118,8 +118,9 @@ __global__ void __launch_bounds__(W * 64, 4) qfc_rows_kernel(QfcArgs a) {
 
 // Fragment form: x lies in memory as the matrix instructions read it (qfc_gather_kernel), NT * 16 batch columns.  No LDS but
 // for the sums.  What bounds it: the copy's launch (2-4 us of the whole) and, from batch 32 on, x out of the L2 caches, which
-// every strip reads (4096x4096 fp16 batch 64: 134 MB of x against 9 of weights, 15.5 us; 8-bit 12.2); two strips per item
-// halve that where 256 items are left (16384x8192, batch 64, 80 -> 55 us).
+// every strip reads (4096x4096 fp16 batch 64: 134 MB of x against 9 of weights, 15.5 us), and the words of y, each a request of its
+// own (50 % kept, 8-bit, batch 64: 255 thousand beside 300 thousand reads, 8.9 us, vector units busy 20 % of the time); two strips
+// per item halve the reads where 256 items are left (16384x8192, batch 64, 80 -> 55 us).
 template <bool Q8, int GPK, bool ZP, int NT, int RS, int W>
 __global__ void __launch_bounds__(W * 64) qfc_frag_kernel(QfcArgs a) {
     extern __shared__ __align__(16) char smem[];
