@@ -200,8 +200,11 @@ def _prepare_norm(c, seed):
     s.scale = torch.zeros(rows, device="cuda") if c["out"] == "q8" else None
     s.p = None
     if own and c["perm"]:         # the layer whose input the rows become: its column permutation is the order they are left in
-        z = dict(bh=16, bw=32, group=32, kept=0.0, zeros=False)
-        s.p, = s.plans([s.layer(16, cols, z, False, pcol=s.pcol)])
+        from paper_1712_01084_amd import binding as B
+        ng = -(-cols // 32)       # (a layer of no tiles: its weights are not read)
+        s.p = B.pivot_qfc_plan(16, cols, 16, 32, 32, np.zeros((16, -(-cols // 2)), np.uint8), np.zeros((16, ng), np.float16),
+                               tile_mask=np.zeros((1, ng), np.uint8), pcol=s.pcol, device=0)
+        s.free.append((B.pivot_qfc_plan_destroy, s.p))
     return s
 
 
